@@ -71,6 +71,59 @@ ls_status lsk_norm_bwd(int kind, const void* dh, int dh_dtype, const float* x,
 ls_status lsk_rope(void* qkv, int dtype, int T, int n_heads, int head_dim, const int32_t* pos,
                    const float* table, float sign, void* stream);
 
+/*
+ * Rotary tables: table [dev] fp32 [n_pos][rot_dim/2][cos, sin] of the angles p * f_i, f_i = theta^(-2i/rot_dim), for
+ * lsk_rope (rot_dim = head_dim), lsk_rope_kv_write, lsk_finish_qkv and the calls below.  scaling [host, null: plain]
+ * stretches the angles for contexts longer than the weights were trained for:
+ *   LSK_ROPE_LINEAR  f_i / factor
+ *   LSK_ROPE_BASE    theta * factor^(rot_dim / (rot_dim - 2)) in place of theta: the slowest pair turns factor times slower,
+ *                    the fastest as before
+ *   LSK_ROPE_PARTS   with n_i = orig_len f_i / (2 pi) turns over the trained length and g = (n_i - beta_slow) /
+ *                    (beta_fast - beta_slow) clamped to 0..1: f_i (g + (1 - g) / factor) (YaRN, section 3.2)
+ * cos and sin are multiplied by magnitude (1: none; YaRN, section 3.4).  factor >= 1.  Angles are computed in 64 bits.
+ * rot_dim even, 2..512.
+ */
+enum { LSK_ROPE_PLAIN = 0, LSK_ROPE_LINEAR = 1, LSK_ROPE_BASE = 2, LSK_ROPE_PARTS = 3 };
+typedef struct {
+  int32_t kind;
+  float factor;
+  int32_t orig_len;            /* LSK_ROPE_PARTS only, as the two below */
+  float beta_fast, beta_slow;
+  float magnitude;
+} lsk_rope_scaling;
+ls_status lsk_rope_table(float* table, int n_pos, int rot_dim, float theta, const lsk_rope_scaling* scaling, void* stream);
+
+/*
+ * Norms of queries and keys for each head with the rotation in the same pass.  in, out [dev] hold rows of
+ * q | k | v = (n_heads + 2 n_kv_heads) * head_dim elements of dtype, ld_in and ld_out elements apart; n_heads is a multiple
+ * of n_kv_heads.  For every head vector x of q and k:
+ *   u = x / sqrt(mean(x^2) + eps) * gain   (kind 1; gain_q / gain_k [dev] [head_dim] of p_dtype, null: 1)   or x (kind -1)
+ *   the first rot_dim elements of u are turned by pos[t] (0: no rotation; pos and table may be null then)
+ * and v is copied.  out may be in (equal ld; v stays) but must not overlap it otherwise.  layout LSK_ROPE_HALF: the pairs
+ * (i, i + rot_dim/2), as lsk_rope; LSK_ROPE_NEIGHBOURS: (2i, 2i + 1).  table [dev] [max_pos][rot_dim/2][cos, sin];
+ * positions outside 0..max_pos-1 take the nearest row.  head_dim even, 2..512; rot_dim even, at most head_dim.  fp32
+ * arithmetic, one rounding.  head_dim and rot_dim multiples of 8 with rows and bases aligned to four elements take the
+ * vectorised kernels.
+ */
+enum { LSK_ROPE_HALF = 0, LSK_ROPE_NEIGHBOURS = 1 };
+ls_status lsk_qk_norm_rope(const void* in, long ld_in, void* out, long ld_out, int dtype, int T, int n_heads,
+                           int n_kv_heads, int head_dim, int kind, const void* gain_q, const void* gain_k, int p_dtype,
+                           float eps, int rot_dim, int layout, const int32_t* pos, const float* table, int max_pos,
+                           void* stream);
+/*
+ * Backward of the above: din (rows of q | k | v) from dout and the forward's input `in` (may be null for kind -1).  din may
+ * be dout (equal ld; v stays), must not overlap it otherwise and never overlaps `in`.  dgain_q, dgain_k [dev] fp32
+ * [head_dim], both or neither (null): (accumulate ? old : 0) + alpha * the gains' gradients, summed over rows and heads in
+ * a fixed order; alpha_dev [dev] as in the *_scaled calls (null = 1).  partial [dev]: fp32 scratch of
+ * lsk_qk_norm_rope_bwd_partial_floats(T, n_heads, n_kv_heads, head_dim) elements (null without dgain_q).
+ */
+size_t lsk_qk_norm_rope_bwd_partial_floats(int T, int n_heads, int n_kv_heads, int head_dim);
+ls_status lsk_qk_norm_rope_bwd(const void* dout, long ld_dout, const void* in, long ld_in, void* din, long ld_din, int dtype,
+                               int T, int n_heads, int n_kv_heads, int head_dim, int kind, const void* gain_q,
+                               const void* gain_k, int p_dtype, float eps, int rot_dim, int layout, const int32_t* pos,
+                               const float* table, int max_pos, float* dgain_q, float* dgain_k, int accumulate,
+                               const float* alpha_dev, float* partial, void* stream);
+
 /* GELU forward g = GELU(u) and backward du = dg * GELU'(u); kind = ls_act. */
 ls_status lsk_gelu_fwd(const void* u, void* g, int dtype, size_t n, int kind, void* stream);
 ls_status lsk_gelu_bwd(const void* dg, const void* u, void* du, int dtype, size_t n, int kind,
@@ -145,6 +198,24 @@ ls_status lsk_kv_reload(const ls_config* cfg, const ls_kv* kv, int request, int 
                         const void* host, void* staging, void* stream);
 ls_status lsk_memory_available(size_t need_bytes, size_t threshold_bytes, int* available,
                                size_t* used_bytes);
+
+/*
+ * Moving cached K/V inside the pools, all layers in one launch; cfg gives the pool's layout (n_layers, n_heads as key heads,
+ * head_dim, page_size, mma_dtype), kv the pools, n_pages and, for rows, block_table, max_pages_per_req and ctx_len.
+ *
+ * lsk_kv_copy_pages: page src[i] -> page dst[i], i < n (src, dst [host], read before the call returns): the copies that
+ * forks and compactions ask for (ls_pages_grow, ls_pages_compact).  LS_EINVAL when a page is outside the pool, written
+ * twice, or both read and written.
+ *
+ * lsk_kv_move_rows: accepts a path of each request's drafted tree: the rows of nodes path[b][i], i < n_path[b]
+ * (path [dev] [B][max_path], n_path [dev] [B]), move from slot ctx_len[b] + path[b][i] to ctx_len[b] + i, so that the
+ * context can be advanced by n_path[b].  Nodes rise along a path; a path is cut at the first node that does not, or whose
+ * slot is beyond the block-table row.  Rows on pages whose id is outside 0..n_pages-1 are skipped.
+ */
+ls_status lsk_kv_copy_pages(const ls_config* cfg, const ls_kv* kv, const int32_t* src, const int32_t* dst, int n,
+                            void* stream);
+ls_status lsk_kv_move_rows(const ls_config* cfg, const ls_kv* kv, int B, const int32_t* path, int max_path,
+                           const int32_t* n_path, void* stream);
 
 /*
  * The update of one parameter tensor of n elements (see stage_optimizer_step
@@ -257,6 +328,51 @@ ls_status lsk_attn_paged_noalloc(const void* qkv, int dtype, int T, int n_heads,
                                  int page_size, int max_ctx, void* o, void* stream);
 
 /*
+ * The serving form of lsk_qk_norm_rope: q goes to q_out [dev] (rows ld_q elements apart; may be qkv with ld_q = ld), the k
+ * and v rows to slot slot[t] (null: pos[t]) of request req[t]'s pages, pools [n_pages][n_kv_heads][page_size][head_dim] of
+ * dtype; k and v of qkv stay as they are.  The slot differs from the position for drafted tokens: nodes of one depth share
+ * a position.  Rows with req[t] < 0 are padding and are skipped; K and V of a slot beyond the block-table row, or of a page
+ * id outside 0..n_pages-1, are not written.  No two rows may share a slot.
+ */
+ls_status lsk_qk_norm_rope_kv_write(const void* qkv, long ld, void* q_out, long ld_q, int dtype, int T, int n_heads,
+                                    int n_kv_heads, int head_dim, int kind, const void* gain_q, const void* gain_k,
+                                    int p_dtype, float eps, int rot_dim, int layout, const int32_t* pos, const float* table,
+                                    int max_pos, const int32_t* req, const int32_t* slot, void* k_pool, void* v_pool,
+                                    const int32_t* block_table, int max_pages_per_req, int page_size, int n_pages,
+                                    void* stream);
+
+/*
+ * Attention for trees of drafted tokens over the paged cache (speculative decoding: the continuations drafted for a request
+ * are verified in one forward).  Request b's tree has start[b+1] - start[b] nodes, 0 up to max_nodes <= 256, which are the
+ * rows start[b] .. start[b+1]-1 (start [dev] [B+1], start[0] = 0, not falling); its node i is at depth d_i: position
+ * ctx_len[b] + d_i, page slot ctx_len[b] + i.  A node's parent comes before it.
+ *
+ * lsk_tree_index computes what the other calls take: from parent [dev] [T] (index within the request's tree, -1: the
+ * context; anything else that is not an earlier node counts as -1) the rows' pos, slot, req [dev] [T] and
+ * mask [dev] [T][ceil(max_nodes/64)], bit j of node i: node j is i or an ancestor of i.  Rows from start[B] to T-1, and
+ * nodes from max_nodes on, become padding: req -1, mask 0.
+ *
+ * lsk_attn_tree: o[t] = softmax over the keys that row t sees of (q[t] k / sqrt(head_dim)) v, where node i of request b
+ * sees the ctx_len[b] cached tokens and node j (slot ctx_len[b] + j) where bit j of its mask is set; any mask will do, and a
+ * row that sees nothing becomes zero.  K and V of the nodes must have been written (lsk_qk_norm_rope_kv_write).  q, o [dev]:
+ * rows of n_heads * head_dim elements, ldq and ldo apart; query head i reads key head i / (n_heads / n_kv_heads).  Keys
+ * beyond the block-table row or of a page id outside 0..n_pages-1 are not seen.  Slots that no row sees, and keys of nodes
+ * that a row does not see, may hold any bit pattern.  Rows from start[B] on, and nodes from max_nodes on, are left as they were.
+ * max_ctx [host]: the largest ctx_len, for launch sizing.  scratch [dev]: fp32 for the partial results of contexts that are
+ * split over workgroups; lsk_attn_tree_scratch_floats gives the most a call uses, fewer (scratch_floats; 0 with null) mean
+ * fewer parts.  head_dim up to 256; 16-bit data with head_dim 32, 64 or 128, page_size a power of two, and q, pools and rows
+ * aligned to 16 bytes takes the matrix-core kernel.  Two calls that overlap in time need two scratches.
+ */
+ls_status lsk_tree_index(const int32_t* parent, const int32_t* start, const int32_t* ctx_len, int B, int T, int max_nodes,
+                         int32_t* pos, int32_t* slot, int32_t* req, uint64_t* mask, void* stream);
+size_t lsk_attn_tree_scratch_floats(int T, int B, int n_heads, int n_kv_heads, int head_dim, int max_nodes, int max_ctx);
+ls_status lsk_attn_tree(const void* q, long ldq, int dtype, int T, int B, int max_nodes, int n_heads, int n_kv_heads,
+                        int head_dim, const int32_t* start, const int32_t* ctx_len, const uint64_t* mask,
+                        const void* k_pool, const void* v_pool, const int32_t* block_table, int max_pages_per_req,
+                        int page_size, int n_pages, int max_ctx, void* o, long ldo, float* scratch, size_t scratch_floats,
+                        void* stream);
+
+/*
  * Backward-pass gradient scaling.  stage_train_bwd runs the whole backward on
  * dY * 2^e so that 16-bit gradient operands stay in the fp16 normal range (the
  * matrix cores flush fp16 subnormal inputs), and multiplies every fp32 result by
@@ -365,7 +481,7 @@ enum {
                                 in an lsk_finish_*) */
   LSK_TIMED_ATTN_FWD = 1,    /* matrix-core attention forward (training and prompt chunks) */
   LSK_TIMED_ATTN_BWD = 2,    /* matrix-core attention backward (all its kernels) */
-  LSK_TIMED_DECODE_ATTN = 3, /* the paged decode-attention kernel and its merge */
+  LSK_TIMED_DECODE_ATTN = 3, /* the paged decode-attention kernel and its merge, and lsk_attn_tree */
   LSK_TIMED_DECODE_GEMM = 4, /* the same of fewer rows, and the projections of decode batches: lsk_gemm_partials, and the matrix-vector
                                 kernels of calls of a few rows with the steps that run inside them */
   LSK_TIMED_FINISH = 5,      /* lsk_finish_* */

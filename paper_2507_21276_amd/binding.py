@@ -57,6 +57,15 @@ class ls_kv(C.Structure):
                 ("n_pages", C.c_int32), ("max_pages_per_req", C.c_int32)]
 
 
+LSK_ROPE_PLAIN, LSK_ROPE_LINEAR, LSK_ROPE_BASE, LSK_ROPE_PARTS = 0, 1, 2, 3
+LSK_ROPE_HALF, LSK_ROPE_NEIGHBOURS = 0, 1
+
+
+class lsk_rope_scaling(C.Structure):
+    _fields_ = [("kind", C.c_int32), ("factor", C.c_float), ("orig_len", C.c_int32), ("beta_fast", C.c_float),
+                ("beta_slow", C.c_float), ("magnitude", C.c_float)]
+
+
 _lib: Optional[C.CDLL] = None
 
 # name -> (restype, argtypes); every symbol the two headers declare
@@ -124,6 +133,19 @@ SIGNATURES = {
     "lsk_finish_resid_norm": (_I, [_VP, _I, _I, _I, _VP, _VP, _VP, _I, _VP, _VP, _I, _F, _VP, _I, _VP]),
     "lsk_finish_act": (_I, [_VP, _I, _I, _I, _I, _VP, _I, _VP, _I, _VP]),
     "lsk_finish_qkv": (_I, [_VP, _I, _I, _I, _I, _VP, _I, _VP, _VP, _VP, _VP, _I, _VP, _VP, _VP, _I, _I, _VP]),
+    "lsk_rope_table": (_I, [_VP, _I, _I, _F, C.POINTER(lsk_rope_scaling), _VP]),
+    "lsk_qk_norm_rope": (_I, [_VP, _L, _VP, _L, _I, _I, _I, _I, _I, _I, _VP, _VP, _I, _F, _I, _I, _VP, _VP, _I, _VP]),
+    "lsk_qk_norm_rope_bwd_partial_floats": (_SZ, [_I, _I, _I, _I]),
+    "lsk_qk_norm_rope_bwd": (_I, [_VP, _L, _VP, _L, _VP, _L, _I, _I, _I, _I, _I, _I, _VP, _VP, _I, _F, _I, _I, _VP, _VP, _I,
+                                  _VP, _VP, _I, _VP, _VP, _VP]),
+    "lsk_qk_norm_rope_kv_write": (_I, [_VP, _L, _VP, _L, _I, _I, _I, _I, _I, _I, _VP, _VP, _I, _F, _I, _I, _VP, _VP, _I,
+                                       _VP, _VP, _VP, _VP, _VP, _I, _I, _I, _VP]),
+    "lsk_tree_index": (_I, [_VP, _VP, _VP, _I, _I, _I, _VP, _VP, _VP, _VP, _VP]),
+    "lsk_attn_tree_scratch_floats": (_SZ, [_I, _I, _I, _I, _I, _I, _I]),
+    "lsk_attn_tree": (_I, [_VP, _L, _I, _I, _I, _I, _I, _I, _I, _VP, _VP, _VP, _VP, _VP, _VP, _I, _I, _I, _I, _VP, _L, _VP,
+                           _SZ, _VP]),
+    "lsk_kv_copy_pages": (_I, [C.POINTER(ls_config), C.POINTER(ls_kv), C.POINTER(C.c_int32), C.POINTER(C.c_int32), _I, _VP]),
+    "lsk_kv_move_rows": (_I, [C.POINTER(ls_config), C.POINTER(ls_kv), _I, _VP, _I, _VP, _VP]),
     # lemix_sched.h (host bookkeeping; wrappers in sched.py)
     "ls_node_create": (_I, [_I, _D, _D, C.POINTER(_VP)]),
     "ls_node_destroy": (None, [_VP]),
@@ -217,14 +239,26 @@ class KV:
         self.n_pages = n_pages
         self.set_ctx(ctx_len, device)
 
+    @classmethod
+    def of(cls, k_pool, v_pool, block_table=None, ctx_len=None):
+        """The descriptor's owner over pools that exist already; without a table or lengths those fields are null."""
+        kv = cls.__new__(cls)
+        kv.stage, kv.k_pool, kv.v_pool, kv.n_pages = None, k_pool, v_pool, k_pool.shape[1]
+        assert k_pool.is_contiguous() and v_pool.is_contiguous() and k_pool.shape == v_pool.shape
+        kv.block_table = None if block_table is None else block_table.contiguous()
+        kv.ctx_host = kv.ctx_len = None
+        if ctx_len is not None:
+            kv.set_ctx(ctx_len, k_pool.device)
+        return kv
+
     def set_ctx(self, ctx_len, device="cuda"):
         self.ctx_host = torch.as_tensor(ctx_len, dtype=torch.int32).contiguous().clone()
         self.ctx_len = self.ctx_host.to(device)
 
     def desc(self, with_host=True) -> ls_kv:
-        return ls_kv(self.k_pool.data_ptr(), self.v_pool.data_ptr(), self.block_table.data_ptr(),
-                     self.ctx_len.data_ptr(), self.ctx_host.data_ptr() if with_host else None,
-                     self.n_pages, self.block_table.shape[1])
+        return ls_kv(self.k_pool.data_ptr(), self.v_pool.data_ptr(), _p(self.block_table), _p(self.ctx_len),
+                     _p(self.ctx_host) if with_host else None, self.n_pages,
+                     0 if self.block_table is None else self.block_table.shape[1])
 
 
 class Stage:
@@ -561,3 +595,114 @@ def lsk_finish_qkv(partial, splits, n_heads, head_dim, pos, req, table, qkv, k_p
                                 CODE_OF_TORCH[bias.dtype] if bias is not None else 0, _p(pos), _p(req), _opt(table),
                                 _p(qkv), CODE_OF_TORCH[qkv.dtype], _p(k_pool), _p(v_pool), _p(block_table),
                                 block_table.shape[1], page_size, _stream(stream)))
+
+
+# ---- the cache path of drafted tokens ------------------------------------------------------------
+
+def _rows(t):
+    """Pointer and row distance of a matrix whose rows are dense."""
+    assert t.dim() == 2 and (t.shape[1] == 1 or t.stride(1) == 1), "rows must be dense"
+    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+def _norm_rope(head_dim, gain_q, gain_k, norm, eps, pos, table, layout):
+    """The arguments that the forms of lsk_qk_norm_rope share, from kind on."""
+    gain = gain_q if gain_q is not None else gain_k
+    assert gain_q is None or gain_q.numel() == head_dim
+    assert gain_k is None or (gain_k.numel() == head_dim and gain_k.dtype == gain.dtype)
+    assert table is None or (table.dtype == torch.float32 and pos is not None and pos.dtype == torch.int32)
+    return (1 if norm else -1, _opt(gain_q), _opt(gain_k), CODE_OF_TORCH[gain.dtype] if gain is not None else 0, eps,
+            2 * table.shape[1] if table is not None else 0, layout, _opt(pos), _opt(table),
+            table.shape[0] if table is not None else 0)
+
+
+def lsk_rope_table(table, theta, scaling=None, stream=None):
+    """Fills table [n_pos, rot_dim / 2, 2] with cos and sin."""
+    assert table.dtype == torch.float32 and table.dim() == 3 and table.shape[2] == 2
+    _check(lib().lsk_rope_table(_p(table), table.shape[0], 2 * table.shape[1], theta,
+                                C.byref(scaling) if scaling is not None else None, _stream(stream)))
+
+
+def lsk_qk_norm_rope(qkv, out, n_heads, n_kv_heads, head_dim, *, gain_q=None, gain_k=None, norm=True, eps=1e-5, pos=None,
+                     table=None, layout=LSK_ROPE_HALF, stream=None):
+    """out = norm and rotation of q and k, and v, of qkv [T, (n_heads + 2 n_kv_heads) head_dim]; table [.., rot_dim / 2, 2]."""
+    assert qkv.shape == out.shape and qkv.dtype == out.dtype and qkv.shape[1] == (n_heads + 2 * n_kv_heads) * head_dim
+    assert pos is None or pos.numel() >= qkv.shape[0]
+    _check(lib().lsk_qk_norm_rope(*_rows(qkv), *_rows(out), CODE_OF_TORCH[qkv.dtype], qkv.shape[0], n_heads, n_kv_heads, head_dim,
+                                  *_norm_rope(head_dim, gain_q, gain_k, norm, eps, pos, table, layout), _stream(stream)))
+
+
+def lsk_qk_norm_rope_bwd(dout, qkv, din, n_heads, n_kv_heads, head_dim, *, gain_q=None, gain_k=None, norm=True, eps=1e-5,
+                         pos=None, table=None, layout=LSK_ROPE_HALF, dgain_q=None, dgain_k=None, accumulate=False, alpha=None,
+                         stream=None):
+    """din from dout and the forward's input; dgain_q, dgain_k (fp32, both or neither) (+)= alpha * the gains' gradients."""
+    assert dout.shape == din.shape and dout.dtype == din.dtype and dout.shape[1] == (n_heads + 2 * n_kv_heads) * head_dim
+    assert qkv is None or (qkv.shape == dout.shape and qkv.dtype == dout.dtype)
+    assert pos is None or pos.numel() >= dout.shape[0]
+    T, partial = dout.shape[0], None
+    for g in (dgain_q, dgain_k):
+        assert g is None or (g.dtype == torch.float32 and g.numel() == head_dim)
+    if dgain_q is not None:
+        n = lib().lsk_qk_norm_rope_bwd_partial_floats(T, n_heads, n_kv_heads, head_dim)
+        partial = torch.empty(n, dtype=torch.float32, device=dout.device)
+    _check(lib().lsk_qk_norm_rope_bwd(*_rows(dout), *(_rows(qkv) if qkv is not None else (None, 0)), *_rows(din),
+                                      CODE_OF_TORCH[dout.dtype], T, n_heads, n_kv_heads, head_dim,
+                                      *_norm_rope(head_dim, gain_q, gain_k, norm, eps, pos, table, layout), _opt(dgain_q),
+                                      _opt(dgain_k), int(accumulate), _opt(alpha), _opt(partial), _stream(stream)))
+
+
+def lsk_qk_norm_rope_kv_write(qkv, q_out, n_heads, n_kv_heads, head_dim, pos, req, k_pool, v_pool, block_table, page_size, *,
+                              slot=None, gain_q=None, gain_k=None, norm=True, eps=1e-5, table=None, layout=LSK_ROPE_HALF,
+                              stream=None):
+    """q of qkv, normalised and rotated, to q_out; k and v to their slots of the pools [n_pages, n_kv_heads, page, head_dim]."""
+    T = qkv.shape[0]
+    assert qkv.dtype == q_out.dtype == k_pool.dtype == v_pool.dtype and qkv.shape[1] == (n_heads + 2 * n_kv_heads) * head_dim
+    assert q_out.shape[0] == T and q_out.shape[1] >= n_heads * head_dim
+    assert k_pool.shape == v_pool.shape and tuple(k_pool.shape[1:]) == (n_kv_heads, page_size, head_dim)
+    assert req.numel() >= T and all(t is None or t.numel() >= T for t in (pos, slot))
+    _check(lib().lsk_qk_norm_rope_kv_write(*_rows(qkv), *_rows(q_out), CODE_OF_TORCH[qkv.dtype], T, n_heads, n_kv_heads, head_dim,
+                                           *_norm_rope(head_dim, gain_q, gain_k, norm, eps, pos, table, layout), _p(req),
+                                           _opt(slot), _p(k_pool), _p(v_pool), _p(block_table), block_table.shape[1], page_size,
+                                           k_pool.shape[0], _stream(stream)))
+
+
+def lsk_tree_index(parent, start, ctx_len, max_nodes, pos, slot, req, mask, stream=None):
+    """pos, slot, req [T] and mask [T, ceil(max_nodes / 64)] (64-bit words) of the trees that parent [T] and start [B + 1] give."""
+    T = pos.numel()
+    assert parent.numel() >= T and slot.numel() >= T and req.numel() >= T and mask.shape == (T, (max_nodes + 63) // 64)
+    assert mask.element_size() == 8 and all(t.dtype == torch.int32 for t in (parent, start, ctx_len, pos, slot, req))
+    _check(lib().lsk_tree_index(_p(parent), _p(start), _p(ctx_len), start.numel() - 1, T, max_nodes, _p(pos), _p(slot), _p(req),
+                                _p(mask), _stream(stream)))
+
+
+def lsk_attn_tree(q, o, n_heads, n_kv_heads, head_dim, start, ctx_len, mask, max_nodes, k_pool, v_pool, block_table, page_size,
+                  max_ctx, scratch=None, stream=None):
+    """o [T, n_heads head_dim] of the drafted trees' rows q over the pools [n_pages, n_kv_heads, page, head_dim]."""
+    T, B = q.shape[0], start.numel() - 1
+    assert q.dtype == o.dtype == k_pool.dtype == v_pool.dtype and o.shape[0] == T and mask.shape == (T, (max_nodes + 63) // 64)
+    assert q.shape[1] >= n_heads * head_dim and o.shape[1] >= n_heads * head_dim and mask.element_size() == 8
+    assert k_pool.shape == v_pool.shape and tuple(k_pool.shape[1:]) == (n_kv_heads, page_size, head_dim)
+    if scratch is None:
+        n = lib().lsk_attn_tree_scratch_floats(T, B, n_heads, n_kv_heads, head_dim, max_nodes, max_ctx)
+        scratch = torch.empty(n, dtype=torch.float32, device=q.device) if n else None
+    _check(lib().lsk_attn_tree(*_rows(q), CODE_OF_TORCH[q.dtype], T, B, max_nodes, n_heads, n_kv_heads, head_dim, _p(start),
+                               _p(ctx_len), _p(mask), _p(k_pool), _p(v_pool), _p(block_table), block_table.shape[1], page_size,
+                               k_pool.shape[0], max_ctx, *_rows(o), _opt(scratch),
+                               scratch.numel() if scratch is not None else 0, _stream(stream)))
+
+
+def lsk_kv_copy_pages(config, kv, src, dst, stream=None):
+    """Pages src[i] -> dst[i] (host integers) of all layers; config: the pool's ls_config."""
+    n = len(src)
+    assert len(dst) == n
+    d = kv.desc(False)
+    a, b = (C.c_int32 * max(1, n))(*src), (C.c_int32 * max(1, n))(*dst)
+    _check(lib().lsk_kv_copy_pages(C.byref(config), C.byref(d), a, b, n, _stream(stream)))
+
+
+def lsk_kv_move_rows(config, kv, path, n_path, stream=None):
+    """Rows of the accepted nodes path [B, max_path] (n_path [B] of them) of every request to the end of its context."""
+    assert path.dtype == n_path.dtype == torch.int32 and n_path.numel() == path.shape[0]
+    d = kv.desc(False)
+    _check(lib().lsk_kv_move_rows(C.byref(config), C.byref(d), path.shape[0], _p(path), path.shape[1], _p(n_path),
+                                  _stream(stream)))

@@ -1,0 +1,371 @@
+// Norms of queries and keys for each head with the rotation in the same pass, its backward, its page-writing form for
+// serving, and the tables of angles.
+//
+// A head vector x of dh elements becomes y = R (g * x r), r = (mean(x^2) + eps)^-1/2: r is one sum over the head's lanes, and
+// R turns pairs of the first rot elements by the row's angles.  Backward, with dy the gradient of y: du = R^T dy,
+//   dg = sum over rows and heads of du * x r,   dx = r (g du - x r^2 S / dh),   S = sum(g du x).
+#include <math.h>
+
+#include "common.h"
+
+namespace {
+
+struct Shape {
+  int T, h, hk, dh, rot;
+  int norm;              // 1: RMSNorm, else none
+  float eps;
+  const void *gain_q, *gain_k;
+  int pdt;
+  const int32_t* pos;
+  const float* table;    // [max_pos][rot / 2][2]
+  int max_pos;
+};
+
+// Where the K and V rows of a serving batch go
+struct Pages {
+  void *k_pool, *v_pool;
+  const int32_t *req, *slot, *block_table;
+  int max_pages, page, n_pages;
+};
+
+// element offset of a row's slot in a pool [n_pages][hk][page][dh], head 0; -1: a padded row, or nowhere in the pool
+__device__ __forceinline__ long slot_of(const Pages& pg, int t, int hk, int dh) {
+  const int r = pg.req[t], s = pg.slot[t];
+  if (r < 0 || s < 0 || s / pg.page >= pg.max_pages) return -1;
+  const int id = pg.block_table[(size_t)r * pg.max_pages + s / pg.page];
+  if ((unsigned)id >= (unsigned)pg.n_pages) return -1;
+  return ((long)id * hk * pg.page + s % pg.page) * dh;
+}
+
+// Pair p < dh / 2 of a head: two element indexes; pairs from rot / 2 on are not turned.
+template <int LAYOUT> __device__ __forceinline__ void pair_at(int p, int rot, int* a, int* b) {
+  if (LAYOUT == 0 && p < rot / 2) { *a = p; *b = p + rot / 2; }
+  else { *a = 2 * p; *b = 2 * p + 1; }   // neighbours; past the turned part too: rot + 2 (p - rot / 2)
+}
+
+__device__ __forceinline__ const float* angles(const Shape& s, int t) {
+  const int p = min(max(s.pos[t], 0), s.max_pos - 1);
+  return s.table + (size_t)p * s.rot;
+}
+
+enum { OUT_ROWS = 0, IN_PLACE = 1, TO_PAGES = 2 };
+
+// Any even dh up to 512, any alignment: one wavefront per (row, head), a lane holds up to four pairs.
+template <int LAYOUT, int MODE>
+__global__ __launch_bounds__(256) void norm_rope_any_kernel(const void* in, long ld_in, void* out, long ld_out, int dt, Shape s,
+                                                            Pages pg) {
+  const int heads = s.h + s.hk + (MODE == IN_PLACE ? 0 : s.hk);
+  const long item = (long)blockIdx.x * 4 + (threadIdx.x >> 6);
+  const int lane = threadIdx.x & 63;
+  if (item >= (long)s.T * heads) return;
+  const int t = (int)(item / heads), hd = (int)(item % heads);
+  const int part = hd < s.h ? 0 : hd < s.h + s.hk ? 1 : 2;
+  const size_t src = (size_t)t * ld_in + (size_t)hd * s.dh;
+  void* dst_base = out;
+  size_t dst = (size_t)t * ld_out + (size_t)hd * s.dh;
+  if (MODE == TO_PAGES) {
+    if (pg.req[t] < 0) return;
+    if (part > 0) {
+      const long at = slot_of(pg, t, s.hk, s.dh);
+      if (at < 0) return;
+      dst_base = part == 1 ? pg.k_pool : pg.v_pool;
+      dst = (size_t)at + (size_t)(hd - s.h - (part - 1) * s.hk) * pg.page * s.dh;
+    }
+  }
+  float a[4], b[4], sum = 0.f;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int p = lane + 64 * i;
+    a[i] = b[i] = 0.f;
+    if (p < s.dh / 2) {
+      int ia, ib;
+      pair_at<LAYOUT>(p, s.rot, &ia, &ib);
+      a[i] = load_as_f(in, src + ia, dt);
+      b[i] = load_as_f(in, src + ib, dt);
+      sum += a[i] * a[i] + b[i] * b[i];
+    }
+  }
+  const float r = s.norm && part < 2 ? rsqrtf(wave_total(sum) / s.dh + s.eps) : 1.f;
+  const void* gain = part == 0 ? s.gain_q : part == 1 ? s.gain_k : nullptr;
+  const float* cs = s.rot && part < 2 ? angles(s, t) : nullptr;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int p = lane + 64 * i;
+    if (p >= s.dh / 2) break;
+    int ia, ib;
+    pair_at<LAYOUT>(p, s.rot, &ia, &ib);
+    float ua = a[i] * r, ub = b[i] * r;
+    if (gain) { ua *= load_as_f(gain, ia, s.pdt); ub *= load_as_f(gain, ib, s.pdt); }
+    if (cs && p < s.rot / 2) {
+      const float c = cs[2 * p], sn = cs[2 * p + 1], ta = ua * c - ub * sn;
+      ub = ua * sn + ub * c;
+      ua = ta;
+    }
+    store_from_f(dst_base, dst + ia, dt, ua);
+    store_from_f(dst_base, dst + ib, dt, ub);
+  }
+}
+
+// Backward for the same shapes.  blockIdx.y: q, k (v rows are copied where din is not dout); a workgroup's wavefronts walk
+// the part's (row, head) pairs and keep the gains' gradients of their lanes; the workgroup's sum goes to
+// partial[y][blockIdx.x][dh].
+template <int LAYOUT>
+__global__ __launch_bounds__(256) void norm_rope_bwd_any_kernel(const void* dout, long ld_dout, const void* in, long ld_in,
+                                                                void* din, long ld_din, int dt, Shape s, float* partial) {
+  __shared__ float s_dg[4][512];
+  const int part = blockIdx.y, heads = part == 0 ? s.h : s.hk, first = part == 0 ? 0 : part == 1 ? s.h : s.h + s.hk;
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const void* gain = part == 0 ? s.gain_q : part == 1 ? s.gain_k : nullptr;
+  float dga[4] = {0.f, 0.f, 0.f, 0.f}, dgb[4] = {0.f, 0.f, 0.f, 0.f};
+  const long items = (long)s.T * heads;
+  for (long item = (long)blockIdx.x * 4 + wave; item < items; item += (long)gridDim.x * 4) {
+    const int t = (int)(item / heads), hd = first + (int)(item % heads);
+    const size_t at = (size_t)hd * s.dh;
+    const float* cs = s.rot && part < 2 ? angles(s, t) : nullptr;
+    float xa[4], xb[4], da[4], db[4], ga[4], gb[4], sq = 0.f, dot = 0.f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int p = lane + 64 * i;
+      xa[i] = xb[i] = da[i] = db[i] = 0.f;
+      ga[i] = gb[i] = 1.f;
+      if (p < s.dh / 2) {
+        int ia, ib;
+        pair_at<LAYOUT>(p, s.rot, &ia, &ib);
+        da[i] = load_as_f(dout, (size_t)t * ld_dout + at + ia, dt);
+        db[i] = load_as_f(dout, (size_t)t * ld_dout + at + ib, dt);
+        if (cs && p < s.rot / 2) {
+          const float c = cs[2 * p], sn = cs[2 * p + 1], ta = da[i] * c + db[i] * sn;
+          db[i] = db[i] * c - da[i] * sn;
+          da[i] = ta;
+        }
+        if (gain) { ga[i] = load_as_f(gain, ia, s.pdt); gb[i] = load_as_f(gain, ib, s.pdt); }
+        if (s.norm && part < 2) {
+          xa[i] = load_as_f(in, (size_t)t * ld_in + at + ia, dt);
+          xb[i] = load_as_f(in, (size_t)t * ld_in + at + ib, dt);
+          sq += xa[i] * xa[i] + xb[i] * xb[i];
+          dot += da[i] * ga[i] * xa[i] + db[i] * gb[i] * xb[i];
+        }
+      }
+    }
+    float r = 1.f, back = 0.f;
+    if (s.norm && part < 2) {
+      r = rsqrtf(wave_total(sq) / s.dh + s.eps);
+      back = wave_total(dot) * r * r / s.dh;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int p = lane + 64 * i;
+      if (p >= s.dh / 2) break;
+      int ia, ib;
+      pair_at<LAYOUT>(p, s.rot, &ia, &ib);
+      dga[i] += da[i] * xa[i] * r;
+      dgb[i] += db[i] * xb[i] * r;
+      store_from_f(din, (size_t)t * ld_din + at + ia, dt, r * (da[i] * ga[i] - xa[i] * back));
+      store_from_f(din, (size_t)t * ld_din + at + ib, dt, r * (db[i] * gb[i] - xb[i] * back));
+    }
+  }
+  if (!partial || part == 2) return;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int p = lane + 64 * i;
+    if (p >= s.dh / 2) break;
+    int ia, ib;
+    pair_at<LAYOUT>(p, s.rot, &ia, &ib);
+    s_dg[wave][ia] = dga[i];
+    s_dg[wave][ib] = dgb[i];
+  }
+  __syncthreads();
+  for (int c = threadIdx.x; c < s.dh; c += 256)
+    partial[((size_t)part * gridDim.x + blockIdx.x) * s.dh + c] = s_dg[0][c] + s_dg[1][c] + s_dg[2][c] + s_dg[3][c];
+}
+
+// dgain (+)= alpha * sum over the workgroups, in their order; 64 columns of one part a workgroup, 16 wavefronts
+__global__ __launch_bounds__(1024) void gain_sum_kernel(const float* partial, int blocks, int dh, float* dgq, float* dgk,
+                                                        int accumulate, const float* alpha) {
+  __shared__ float s_sum[16][64];
+  const int part = blockIdx.y, wave = threadIdx.x >> 6, lane = threadIdx.x & 63, c = blockIdx.x * 64 + lane;
+  float v = 0.f;
+  if (c < dh)
+    for (int b = wave; b < blocks; b += 16) v += partial[((size_t)part * blocks + b) * dh + c];
+  s_sum[wave][lane] = v;
+  __syncthreads();
+  if (wave > 0 || c >= dh) return;
+  v = 0.f;
+#pragma unroll
+  for (int w = 0; w < 16; ++w) v += s_sum[w][lane];
+  if (alpha) v *= alpha[0];
+  float* out = part == 0 ? dgq : dgk;
+  out[c] = accumulate ? out[c] + v : v;
+}
+
+// Workgroups of the backward pass: the sums over rows are kept by that many
+int bwd_blocks(long rows_heads) {
+  const long n = (rows_heads + 3) / 4;
+  return (int)(n < 1024 ? n : 1024);
+}
+
+constexpr int kMaxHalf = 256;   // frequencies passed by value
+struct Freqs { double f[kMaxHalf]; };
+
+// table[p][i] = mag * (cos, sin)(p f_i).  A thread takes one frequency and kRun positions: the angle of the first by sincos,
+// the next ones by turning it one step further, in 64 bits (each turn adds less than 2^-52 of error: far below the half step
+// 2^-25 that the result is rounded by), so that the pass is bound by its writes and not by sincos of 64-bit angles.
+constexpr int kRun = 16;
+__global__ __launch_bounds__(256) void rope_table_kernel(float* table, int n_pos, int half, Freqs fr, double mag) {
+  const long idx = (long)blockIdx.x * 256 + threadIdx.x;
+  const int i = (int)(idx % half);
+  const long p0 = idx / half * kRun;
+  if (p0 >= n_pos) return;
+  double c, s, c1, s1;
+  sincos((double)p0 * fr.f[i], &s, &c);
+  sincos(fr.f[i], &s1, &c1);
+  const int n = (int)(n_pos - p0 < kRun ? n_pos - p0 : kRun);
+  for (int k = 0; k < n; ++k) {
+    float* at = table + ((size_t)(p0 + k) * half + i) * 2;
+    at[0] = (float)(mag * c);
+    at[1] = (float)(mag * s);
+    const double t = c * c1 - s * s1;
+    s = s * c1 + c * s1;
+    c = t;
+  }
+}
+
+ls_status check_shape(const char* who, int dt, const Shape& s, int layout) {
+  LS_REQUIRE(dt == LS_F32 || dt == LS_BF16 || dt == LS_F16, "%s: unknown dtype %d", who, dt);
+  LS_REQUIRE(s.T > 0 && s.h > 0 && s.hk > 0, "%s: non-positive size (T %d, heads %d, %d)", who, s.T, s.h, s.hk);
+  LS_REQUIRE(s.h % s.hk == 0, "%s: %d query heads do not share %d key heads evenly", who, s.h, s.hk);
+  LS_REQUIRE(s.dh >= 2 && s.dh <= 512 && s.dh % 2 == 0, "%s: head_dim %d is not even or outside 2..512", who, s.dh);
+  LS_REQUIRE((long)s.T * (s.h + 2L * s.hk) <= 0x7fffffffL * 4, "%s: too many (row, head) pairs", who);
+  LS_REQUIRE(s.norm == -1 || s.norm == 1, "%s: kind %d is neither -1 (no norm) nor 1 (RMSNorm)", who, s.norm);
+  LS_REQUIRE(s.norm == 1 || (!s.gain_q && !s.gain_k), "%s: gains without a norm", who);
+  LS_REQUIRE(s.norm == -1 || s.eps > 0, "%s: eps must be positive", who);
+  LS_REQUIRE(s.pdt == LS_F32 || s.pdt == LS_BF16 || s.pdt == LS_F16, "%s: unknown dtype %d of the gains", who, s.pdt);
+  LS_REQUIRE(s.rot >= 0 && s.rot <= s.dh && s.rot % 2 == 0, "%s: %d rotated elements of %d", who, s.rot, s.dh);
+  LS_REQUIRE(s.rot == 0 || (s.pos && s.table && s.max_pos > 0), "%s: rotation without positions or table", who);
+  LS_REQUIRE(layout == LSK_ROPE_HALF || layout == LSK_ROPE_NEIGHBOURS, "%s: unknown layout %d", who, layout);
+  return LS_OK;
+}
+
+Shape make_shape(int T, int h, int hk, int dh, int kind, const void* gq, const void* gk, int pdt, float eps, int rot,
+                 const int32_t* pos, const float* table, int max_pos) {
+  return Shape{T, h, hk, dh, rot, kind, eps, gq, gk, pdt, pos, table, max_pos};
+}
+
+template <int MODE>
+ls_status launch_fwd(const void* in, long ld_in, void* out, long ld_out, int dt, Shape s, int layout, const Pages& pg,
+                     hipStream_t st) {
+  s.norm = s.norm == 1;
+  const long items = (long)s.T * (s.h + s.hk + (MODE == IN_PLACE ? 0 : s.hk));
+  const unsigned grid = (unsigned)((items + 3) / 4);
+  if (layout == 0) norm_rope_any_kernel<0, MODE><<<grid, 256, 0, st>>>(in, ld_in, out, ld_out, dt, s, pg);
+  else norm_rope_any_kernel<1, MODE><<<grid, 256, 0, st>>>(in, ld_in, out, ld_out, dt, s, pg);
+  LS_CHECK_LAUNCH();
+  return LS_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+ls_status lsk_rope_table(float* table, int n_pos, int rot_dim, float theta, const lsk_rope_scaling* scaling, void* stream) {
+  LS_REQUIRE(table, "rope_table: null table");
+  LS_REQUIRE(n_pos > 0, "rope_table: non-positive number of positions");
+  LS_REQUIRE(rot_dim >= 2 && rot_dim <= 2 * kMaxHalf && rot_dim % 2 == 0, "rope_table: rot_dim %d is not even or outside 2..%d",
+             rot_dim, 2 * kMaxHalf);
+  LS_REQUIRE(theta > 0 && isfinite(theta), "rope_table: theta must be positive and finite");
+  const lsk_rope_scaling plain = {LSK_ROPE_PLAIN, 1.f, 0, 0.f, 0.f, 1.f};
+  const lsk_rope_scaling& sc = scaling ? *scaling : plain;
+  LS_REQUIRE(sc.kind >= LSK_ROPE_PLAIN && sc.kind <= LSK_ROPE_PARTS, "rope_table: unknown scaling %d", sc.kind);
+  LS_REQUIRE(isfinite(sc.magnitude) && sc.magnitude > 0, "rope_table: magnitude must be positive and finite");
+  LS_REQUIRE(sc.kind == LSK_ROPE_PLAIN || (sc.factor >= 1 && isfinite(sc.factor)), "rope_table: factor must be at least 1");
+  LS_REQUIRE(sc.kind != LSK_ROPE_BASE || rot_dim > 2, "rope_table: the base of a single pair has no effect");
+  LS_REQUIRE(sc.kind != LSK_ROPE_PARTS || (sc.orig_len > 0 && sc.beta_fast > sc.beta_slow && sc.beta_slow >= 0),
+             "rope_table: parts need orig_len > 0 and beta_fast > beta_slow >= 0");
+  const int half = rot_dim / 2;
+  Freqs fr;
+  double base = theta;
+  if (sc.kind == LSK_ROPE_BASE) base *= pow((double)sc.factor, (double)rot_dim / (rot_dim - 2));
+  for (int i = 0; i < half; ++i) {
+    double f = pow(base, -2.0 * i / rot_dim);
+    if (sc.kind == LSK_ROPE_LINEAR) f /= sc.factor;
+    if (sc.kind == LSK_ROPE_PARTS) {
+      const double turns = sc.orig_len * f / (2.0 * M_PI);
+      double g = (turns - sc.beta_slow) / ((double)sc.beta_fast - sc.beta_slow);
+      g = g < 0 ? 0 : g > 1 ? 1 : g;
+      f *= g + (1.0 - g) / sc.factor;
+    }
+    fr.f[i] = f;
+  }
+  const long threads = ((long)n_pos + kRun - 1) / kRun * half;
+  rope_table_kernel<<<(unsigned)((threads + 255) / 256), 256, 0, (hipStream_t)stream>>>(table, n_pos, half, fr,
+                                                                                        (double)sc.magnitude);
+  LS_CHECK_LAUNCH();
+  return LS_OK;
+}
+
+ls_status lsk_qk_norm_rope(const void* in, long ld_in, void* out, long ld_out, int dt, int T, int h, int hk, int dh, int kind,
+                           const void* gain_q, const void* gain_k, int p_dtype, float eps, int rot_dim, int layout,
+                           const int32_t* pos, const float* table, int max_pos, void* stream) {
+  const Shape s = make_shape(T, h, hk, dh, kind, gain_q, gain_k, p_dtype, eps, rot_dim, pos, table, max_pos);
+  LS_TRY(check_shape("qk_norm_rope", dt, s, layout));
+  LS_REQUIRE(in && out, "qk_norm_rope: null argument");
+  const long width = (h + 2L * hk) * dh;
+  LS_REQUIRE(ld_in >= width && ld_out >= width, "qk_norm_rope: rows of %ld elements are %ld and %ld apart", width, ld_in, ld_out);
+  LS_REQUIRE(in != out || ld_in == ld_out, "qk_norm_rope: in place, the rows must be equally far apart");
+  const Pages none = {};
+  return in == out ? launch_fwd<IN_PLACE>(in, ld_in, out, ld_out, dt, s, layout, none, (hipStream_t)stream)
+                   : launch_fwd<OUT_ROWS>(in, ld_in, out, ld_out, dt, s, layout, none, (hipStream_t)stream);
+}
+
+ls_status lsk_qk_norm_rope_kv_write(const void* qkv, long ld, void* q_out, long ld_q, int dt, int T, int h, int hk, int dh,
+                                    int kind, const void* gain_q, const void* gain_k, int p_dtype, float eps, int rot_dim,
+                                    int layout, const int32_t* pos, const float* table, int max_pos, const int32_t* req,
+                                    const int32_t* slot, void* k_pool, void* v_pool, const int32_t* block_table,
+                                    int max_pages, int page, int n_pages, void* stream) {
+  const Shape s = make_shape(T, h, hk, dh, kind, gain_q, gain_k, p_dtype, eps, rot_dim, pos, table, max_pos);
+  LS_TRY(check_shape("qk_norm_rope_kv_write", dt, s, layout));
+  LS_REQUIRE(qkv && q_out && req && k_pool && v_pool && block_table, "qk_norm_rope_kv_write: null argument");
+  LS_REQUIRE(pos || slot, "qk_norm_rope_kv_write: neither slots nor positions");
+  LS_REQUIRE(max_pages > 0 && n_pages > 0 && page > 0, "qk_norm_rope_kv_write: non-positive page counts");
+  LS_REQUIRE(ld >= (h + 2L * hk) * dh && ld_q >= (long)h * dh, "qk_norm_rope_kv_write: rows overlap (ld %ld, ld_q %ld)", ld, ld_q);
+  LS_REQUIRE(qkv != q_out || ld == ld_q, "qk_norm_rope_kv_write: in place, the rows must be equally far apart");
+  const Pages pg = {k_pool, v_pool, req, slot ? slot : pos, block_table, max_pages, page, n_pages};
+  return launch_fwd<TO_PAGES>(qkv, ld, q_out, ld_q, dt, s, layout, pg, (hipStream_t)stream);
+}
+
+size_t lsk_qk_norm_rope_bwd_partial_floats(int T, int h, int hk, int dh) {
+  if (T <= 0 || h <= 0 || hk <= 0 || dh <= 0) return 0;
+  return (size_t)2 * bwd_blocks((long)T * h) * dh;
+}
+
+ls_status lsk_qk_norm_rope_bwd(const void* dout, long ld_dout, const void* in, long ld_in, void* din, long ld_din, int dt, int T,
+                               int h, int hk, int dh, int kind, const void* gain_q, const void* gain_k, int p_dtype, float eps,
+                               int rot_dim, int layout, const int32_t* pos, const float* table, int max_pos, float* dgain_q,
+                               float* dgain_k, int accumulate, const float* alpha_dev, float* partial, void* stream) {
+  Shape s = make_shape(T, h, hk, dh, kind, gain_q, gain_k, p_dtype, eps, rot_dim, pos, table, max_pos);
+  LS_TRY(check_shape("qk_norm_rope_bwd", dt, s, layout));
+  LS_REQUIRE(dout && din && (in || kind == -1), "qk_norm_rope_bwd: null argument");
+  const long width = (h + 2L * hk) * dh;
+  LS_REQUIRE(ld_dout >= width && ld_din >= width && (kind == -1 || ld_in >= width),
+             "qk_norm_rope_bwd: rows of %ld elements are %ld, %ld and %ld apart", width, ld_dout, ld_in, ld_din);
+  LS_REQUIRE(din != dout || ld_din == ld_dout, "qk_norm_rope_bwd: in place, the rows must be equally far apart");
+  LS_REQUIRE(din != in, "qk_norm_rope_bwd: din must not be the forward's input");
+  LS_REQUIRE(!dgain_q == !dgain_k, "qk_norm_rope_bwd: one of the gains' gradients is null");
+  LS_REQUIRE(!dgain_q || (gain_q && gain_k), "qk_norm_rope_bwd: gradients of gains that are not there");
+  LS_REQUIRE(!dgain_q || partial, "qk_norm_rope_bwd: null partial");
+  hipStream_t st = (hipStream_t)stream;
+  s.norm = s.norm == 1;
+  const int blocks = bwd_blocks((long)T * h);
+  float* sums = dgain_q ? partial : nullptr;
+  const dim3 grid(blocks, din == dout ? 2 : 3);
+  if (layout == 0) norm_rope_bwd_any_kernel<0><<<grid, 256, 0, st>>>(dout, ld_dout, in, ld_in, din, ld_din, dt, s, sums);
+  else norm_rope_bwd_any_kernel<1><<<grid, 256, 0, st>>>(dout, ld_dout, in, ld_in, din, ld_din, dt, s, sums);
+  LS_CHECK_LAUNCH();
+  if (sums) {
+    gain_sum_kernel<<<dim3((dh + 63) / 64, 2), 1024, 0, st>>>(sums, blocks, dh, dgain_q, dgain_k, accumulate, alpha_dev);
+    LS_CHECK_LAUNCH();
+  }
+  return LS_OK;
+}
+
+}  // extern "C"
