@@ -2,6 +2,8 @@
 // verified by one forward).  The rows of a request are the nodes of its tree; their K and V rows lie in the pages behind the
 // ctx cached tokens, in node order, and node i attends to all cached tokens and to the nodes that its mask names (itself and
 // its ancestors).
+#include <type_traits>
+
 #include "common.h"
 
 namespace {
@@ -138,6 +140,385 @@ __global__ __launch_bounds__(256) void tree_attn_any_kernel(const T* q, long ldq
   }
 }
 
+// ---- 16-bit matrix-core kernel ------------------------------------------------------------------
+//
+// A workgroup of four wavefronts owns 16 NT rows (node, query head of one key head) of one request, one key head and one part
+// of the keys; the wavefronts share out the part's tiles of 32 keys, so that every K and V byte is loaded by one wavefront,
+// straight to registers, and serves all rows.  S^T = K Q^T (16x16x32) leaves a row's scores in one lane column; the lane's
+// eight keys of a tile are 4 q .. 4 q + 3 and 16 + 4 q .. + 3 (q = lane / 16), and O^T += V^T P^T takes P from these very
+// registers when V^T is fed in the same order of keys, which two transposing LDS reads per 16 head dimensions do.  The
+// wavefront writes its V tile to its own LDS buffer for them: no barrier in the loop.
+template <class T> struct Mma16;
+template <> struct Mma16<bf16_t> {
+  typedef bf16x8 V8;
+  static __device__ __forceinline__ f32x4 run(V8 a, V8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+  static constexpr uint32_t kExp = 0x7f80u;   // exponent bits: all set in infinities and NaN
+  static constexpr float kLift = 0.f;
+};
+template <> struct Mma16<f16_t> {
+  typedef f16x8 V8;
+  static __device__ __forceinline__ f32x4 run(V8 a, V8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+  static constexpr uint32_t kExp = 0x7c00u;
+  static constexpr float kLift = 6.f;
+};
+
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef short s16x8 __attribute__((ext_vector_type(8)));
+typedef __fp16 h16x4 __attribute__((ext_vector_type(4)));
+
+// Byte offset of 16-byte piece c of row r in a V tile.  A transposing read takes 32 bytes of each of 16 rows: pairs of pieces
+// are spread over the banks by the row.
+template <int DH> __device__ __forceinline__ int v_at(int r, int c) {
+  constexpr int PAIRS = DH / 16;
+  const int x = DH == 128 ? r & 7 : DH == 64 ? (r >> 1) & 3 : (r >> 2) & 1;
+  return r * (DH * 2) + (((c >> 1) ^ (x & (PAIRS - 1))) << 5) + ((c & 1) << 4);
+}
+
+struct Parts {
+  int n, keys;       // parts of a context, keys of each (the last takes the rest)
+  int row_blocks;
+  float* partial;    // [T][h][n][dh + 2]: output, maximum (base 2), sum
+};
+
+template <class T, int DH, int NT>
+__global__ __launch_bounds__(256, NT == 4 ? 1 : 2) void tree_attn_kernel(const T* __restrict__ q, long ldq, T* __restrict__ o,
+                                                                         long ldo, const T* __restrict__ k_pool,
+                                                                         const T* __restrict__ v_pool,
+                                                                         const int32_t* __restrict__ table,
+                                                                         const uint64_t* __restrict__ masks, Tree tr, int h,
+                                                                         int hk, int shift, float scale_log2, Parts parts) {
+  typedef typename Mma16<T>::V8 V8;
+  constexpr int KS = DH / 32, DT = DH / 16, NL = DH / 16, LPR = DH / 8;   // loads of K, and of V, per tile; lanes per V row
+  constexpr int TILE = 32 * DH * 2, WAVE_LDS = TILE > 2048 * NT ? TILE : 2048 * NT;
+  constexpr int JOIN = 4 * 16 * (DH + 4) * 4;
+  __shared__ __attribute__((aligned(16))) char smem[4 * WAVE_LDS > JOIN ? 4 * WAVE_LDS : JOIN];
+  __shared__ float s_m[4][NT * 16], s_l[4][NT * 16];
+
+  // Blocks of rows that read the same keys follow each other on one XCD (workgroups go round the eight of them)
+  const int slot8 = blockIdx.x >> 3, item = (slot8 / parts.row_blocks) * 8 + (blockIdx.x & 7), rb = slot8 % parts.row_blocks;
+  if (item >= tr.B * hk) return;
+  const int b = item / hk, kvh = item % hk, part = blockIdx.y, g = h / hk;
+  const int first = tr.start[b], nodes = min(min(tr.start[b + 1], tr.T) - first, tr.max_nodes), rows = nodes * g;
+  const int row0 = rb * (16 * NT);
+  if (first < 0 || row0 >= rows) return;
+  const int ctx = max(tr.ctx_len[b], 0), page = 1 << shift;
+  const int nkeys = (int)min((long)ctx + nodes, (long)tr.max_pages * page);
+  const int used = min(parts.n, max(1, (nkeys + parts.keys - 1) / parts.keys));   // parts of this request
+  if (part >= used) return;
+  const int k_lo = part * parts.keys, k_hi = part == used - 1 ? nkeys : k_lo + parts.keys;
+  const int t_lo = k_lo / 32, t_hi = (k_hi + 31) / 32;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, col = lane & 15, quad = lane >> 4;
+  const int32_t* bt = table + (long)b * tr.max_pages;
+  char* vt = smem + wave * WAVE_LDS;
+
+  V8 qf[NT][KS];
+  int node[NT];      // of the lane's row
+#pragma unroll
+  for (int n = 0; n < NT; ++n) {
+    const int r = row0 + n * 16 + col;
+    node[n] = min(r, rows - 1) / g;
+    const T* qr = q + (long)(first + node[n]) * ldq + (long)(kvh * g + (r < rows ? r % g : g - 1)) * DH;
+#pragma unroll
+    for (int s = 0; s < KS; ++s) qf[n][s] = *(const V8*)(qr + s * 32 + quad * 8);
+  }
+  f32x4 oacc[NT][DT];
+  float m_run[NT], l_run[NT];
+#pragma unroll
+  for (int n = 0; n < NT; ++n) {
+    m_run[n] = -INFINITY;
+    l_run[n] = 0.f;
+#pragma unroll
+    for (int j = 0; j < DT; ++j) oacc[n][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+
+  // A tile's rows lie in groups of eight on one page each: their offsets in the pools, and which of them lie on no page
+  struct Where { long at[4]; int bad; };
+  const int last_page = (nkeys - 1) >> shift;
+  auto find = [&](int t, Where& w) {
+    w.bad = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int key = t * 32 + i * 8;
+      int id = bt[min(key >> shift, last_page)];
+      if ((unsigned)id >= (unsigned)tr.n_pages) { id = 0; w.bad |= 1 << i; }
+      w.at[i] = ((((long)id * hk + kvh) << shift) + (key & (page - 1))) * DH;
+    }
+  };
+  auto fetch = [&](const Where& w, V8 (&kf)[NL], V8 (&vf)[NL]) {
+    const int hi8 = (lane >> 3) & 1;
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+      const T* kr = k_pool + (hi8 ? w.at[2 * c + 1] : w.at[2 * c]) + (lane & 7) * DH + quad * 8;
+#pragma unroll
+      for (int s = 0; s < KS; ++s) kf[c * KS + s] = *(const V8*)(kr + s * 32);
+    }
+#pragma unroll
+    for (int j = 0; j < NL; ++j) {
+      const int r = j * (64 / LPR) + lane / LPR;
+      const long at = DH == 128 ? w.at[j >> 1] : DH == 64 ? w.at[j & 3] : (lane >> 5) ? w.at[(2 * j + 1) & 3] : w.at[(2 * j) & 3];
+      vf[j] = *(const V8*)(v_pool + at + (r & 7) * DH + (lane % LPR) * 8);
+    }
+  };
+  auto attend = [&](int t, const V8 (&kf)[NL], const V8 (&vf)[NL], int bad) {
+    const int k0 = t * 32;
+    const bool plain = k0 + 32 <= ctx && k0 + 32 <= k_hi && bad == 0;   // all rows see all keys
+    // V to LDS.  In the tiles that some row does not see whole, values that are not finite are left out of the product (0 * x
+    // would reach the rows that do not see them) and added to the rows that do afterwards.
+    bool odd = false;
+#pragma unroll
+    for (int j = 0; j < NL; ++j) {
+      const int r = j * (64 / LPR) + lane / LPR;
+      u32x4 v = __builtin_bit_cast(u32x4, vf[j]);
+      if (!plain) {
+        const bool live = k0 + r < k_hi && !(bad >> (r >> 3) & 1);
+        constexpr uint32_t E = Mma16<T>::kExp;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const bool lo = (v[e] & E) == E, hi = (v[e] >> 16 & E) == E;
+          odd |= live && (lo || hi);
+          v[e] = !live ? 0u : v[e] & (lo ? 0xffff0000u : ~0u) & (hi ? 0x0000ffffu : ~0u);
+        }
+      }
+      *(u32x4*)(vt + v_at<DH>(r, lane % LPR)) = v;
+    }
+    f32x4 sacc[NT][2];
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        sacc[n][c] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int s = 0; s < KS; ++s) sacc[n][c] = Mma16<T>::run(kf[c * KS + s], qf[n][s], sacc[n][c]);
+      }
+    uint32_t seen[NT];   // bit r: the lane's row sees key k0 + r
+    if (!plain) {
+      uint32_t live = k_hi - k0 >= 32 ? ~0u : (1u << (k_hi - k0)) - 1;
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (bad >> i & 1) live &= ~(0xffu << (8 * i));
+      const int nd0 = k0 - ctx, w0 = nd0 >> 6, sh = nd0 & 63;   // node of the tile's first key; negative: cached tokens come first
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+        const uint64_t* mask = masks + (size_t)(first + node[n]) * tr.words;
+        uint64_t win = 0;
+        if (nd0 <= -32) win = ~0ull;
+        else if (nd0 < 0) win = mask[0] << -nd0 | ((1ull << -nd0) - 1);
+        else if (w0 < tr.words) {
+          win = mask[w0] >> sh;
+          if (sh > 32 && w0 + 1 < tr.words) win |= mask[w0 + 1] << (64 - sh);
+        }
+        seen[n] = (uint32_t)win & live;
+#pragma unroll
+        for (int c = 0; c < 2; ++c)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (!(seen[n] >> (16 * c + 4 * quad + i) & 1)) sacc[n][c][i] = -INFINITY;
+      }
+    }
+    V8 pf[NT];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      float mx = fmaxf(fmaxf(fmaxf(sacc[n][0][0], sacc[n][0][1]), fmaxf(sacc[n][0][2], sacc[n][0][3])),
+                       fmaxf(fmaxf(sacc[n][1][0], sacc[n][1][1]), fmaxf(sacc[n][1][2], sacc[n][1][3])));
+      mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
+      mx = fmaxf(mx, __shfl_xor(mx, 32, 64)) * scale_log2;
+      // The reference of the exponentials follows the maximum only when some row exceeds it by more than 2^8: until then the
+      // weights stay at or below 256, inside every format, and nothing has to be rescaled.
+      if (__builtin_amdgcn_ballot_w64(mx > m_run[n] + 8.f) != 0) {
+        const float m_new = fmaxf(m_run[n], mx);
+        const float alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m_run[n] - m_new);
+        l_run[n] *= alpha;
+        m_run[n] = m_new;
+#pragma unroll
+        for (int j = 0; j < DT; ++j) oacc[n][j] *= alpha;
+      }
+      // fp16 weights are lifted by 2^6, to 2^14 at most: the matrix cores take subnormal operands for zero, and so only
+      // weights below 2^-20 of the largest are lost.  The sums carry the same factor, which the division takes out.
+      const float ref = (m_run[n] == -INFINITY ? 0.f : m_run[n]) - Mma16<T>::kLift;
+#pragma unroll
+      for (int c = 0; c < 2; ++c)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(sacc[n][c][i], scale_log2, -ref));
+          l_run[n] += p;
+          sacc[n][c][i] = p;
+          pf[n][4 * c + i] = from_f<T>(p);   // the second product's operand: 16 bits, relative error of half a step each
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < DT; ++j) {
+      // keys 4 quad + (col / 4), head dimensions 16 j + 4 (col % 4) ..: the lane receives its column of the 4 x 16 block
+      const char* p0 = vt + v_at<DH>(4 * quad + (col >> 2), 2 * j + ((col >> 1) & 1)) + (col & 1) * 8;
+      const char* p1 = vt + v_at<DH>(16 + 4 * quad + (col >> 2), 2 * j + ((col >> 1) & 1)) + (col & 1) * 8;
+      const s16x4 lo = __builtin_bit_cast(s16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                           (__attribute__((address_space(3))) s16x4*)p0));
+      const s16x4 hi = __builtin_bit_cast(s16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                           (__attribute__((address_space(3))) s16x4*)p1));
+      const V8 vfrag = __builtin_bit_cast(V8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+#pragma unroll
+      for (int n = 0; n < NT; ++n) oacc[n][j] = Mma16<T>::run(vfrag, pf[n], oacc[n][j]);
+    }
+    if (!plain && __builtin_amdgcn_ballot_w64(odd) != 0) {
+      // Rare: a value of this tile is infinite or NaN.  The weights go to LDS (-1: not seen), then key by key the values that
+      // were left out are read again and added where they are seen.
+      float* ps = (float*)vt;
+      Where w;
+      find(t, w);
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int c = 0; c < 2; ++c)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            ps[((16 * c + 4 * quad + i) * NT + n) * 16 + col] = seen[n] >> (16 * c + 4 * quad + i) & 1 ? sacc[n][c][i] : -1.f;
+#pragma unroll 1
+      for (int r = 0; r < 32; ++r) {
+        if (k0 + r >= k_hi || (bad >> (r >> 3) & 1)) continue;
+        const long at = r < 8 ? w.at[0] : r < 16 ? w.at[1] : r < 24 ? w.at[2] : w.at[3];
+        const T* vr = v_pool + at + (r & 7) * DH;
+        float p[NT];
+#pragma unroll
+        for (int n = 0; n < NT; ++n) p[n] = ps[(r * NT + n) * 16 + col];
+#pragma unroll
+        for (int j = 0; j < DT; ++j)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const float v = to_f(vr[16 * j + 4 * quad + i]);
+            if (v - v != 0.f) {
+#pragma unroll
+              for (int n = 0; n < NT; ++n)
+                if (p[n] >= 0.f || p[n] != p[n]) oacc[n][j][i] += p[n] * v;
+            }
+          }
+      }
+    }
+  };
+
+  int t = t_lo + wave;
+  if (t < t_hi) {
+    Where w0, w1;
+    V8 k0[NL], v0[NL], k1[NL], v1[NL];
+    find(t, w0);
+    fetch(w0, k0, v0);
+    int bad0 = w0.bad, bad1 = 0;
+    if (t + 4 < t_hi) find(t + 4, w1);
+    for (; t < t_hi; t += 8) {
+      if (t + 4 < t_hi) {
+        fetch(w1, k1, v1);
+        bad1 = w1.bad;
+        if (t + 8 < t_hi) find(t + 8, w0);
+      }
+      attend(t, k0, v0, bad0);
+      if (t + 4 < t_hi) {
+        if (t + 8 < t_hi) {
+          fetch(w0, k0, v0);
+          bad0 = w0.bad;
+          if (t + 12 < t_hi) find(t + 12, w1);
+        }
+        attend(t + 4, k1, v1, bad1);
+      }
+    }
+  }
+  // Join the four wavefronts, 16 rows at a time, through LDS
+#pragma unroll
+  for (int n = 0; n < NT; ++n) {
+    float l = l_run[n] + __shfl_xor(l_run[n], 16, 64);
+    l += __shfl_xor(l, 32, 64);
+    if (quad == 0) { s_m[wave][n * 16 + col] = m_run[n]; s_l[wave][n * 16 + col] = l; }
+  }
+  float* so = (float*)smem;   // [wave][row][DH + 4]
+#pragma unroll
+  for (int n = 0; n < NT; ++n) {
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < DT; ++j) *(f32x4*)(so + (wave * 16 + col) * (DH + 4) + 16 * j + 4 * quad) = oacc[n][j];
+    __syncthreads();
+    const int r = threadIdx.x >> 4, row = row0 + n * 16 + r;   // 16 threads a row
+    if (row < rows) {
+      const float mm = fmaxf(fmaxf(s_m[0][n * 16 + r], s_m[1][n * 16 + r]), fmaxf(s_m[2][n * 16 + r], s_m[3][n * 16 + r]));
+      const float ref = mm == -INFINITY ? 0.f : mm;
+      float f[4], l = 0.f;
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        f[w] = __builtin_amdgcn_exp2f(s_m[w][n * 16 + r] - ref);
+        l += s_l[w][n * 16 + r] * f[w];
+      }
+      const long trow = first + row / g, head = kvh * g + row % g;
+      const float inv = l == 0.f ? 0.f : 1.f / l;   // a row that sees nothing: zeros
+      for (int c = (threadIdx.x & 15) * 4; c < DH; c += 64) {
+        f32x4 v = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+          const f32x4 x = *(const f32x4*)(so + (w * 16 + r) * (DH + 4) + c);
+          // a wavefront without a tile has weight 0 and zeros
+          v += x * f[w];
+        }
+        if (used == 1) {
+          typedef T V4 __attribute__((ext_vector_type(4)));
+          V4 out;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) out[i] = from_f<T>(l == 0.f ? 0.f : v[i] * inv);
+          *(V4*)(o + trow * ldo + head * DH + c) = out;
+        } else {
+          *(f32x4*)(parts.partial + ((trow * h + head) * parts.n + part) * (DH + 4) + c) = v;
+        }
+      }
+      if (used > 1 && (threadIdx.x & 15) == 0) {
+        float* pp = parts.partial + ((trow * h + head) * parts.n + part) * (DH + 4) + DH;
+        pp[0] = mm;
+        pp[1] = l;
+      }
+    }
+  }
+}
+
+// Joins the parts of a (row, head), in their order; a wavefront each
+template <class T, int DH>
+__global__ __launch_bounds__(256) void tree_merge_kernel(T* __restrict__ o, long ldo, Tree tr, int h, int hk, int shift, Parts parts) {
+  const long item = (long)blockIdx.x * 4 + (threadIdx.x >> 6);
+  const int t = (int)(item / h), head = (int)(item % h), lane = threadIdx.x & 63;
+  if (t >= min(tr.start[tr.B], tr.T) || t < tr.start[0]) return;
+  const int b = request_of(tr.start, tr.B, t), first = tr.start[b];
+  const int nodes = min(min(tr.start[b + 1], tr.T) - first, tr.max_nodes);
+  if (t - first >= nodes) return;
+  const int nkeys = (int)min((long)max(tr.ctx_len[b], 0) + nodes, (long)tr.max_pages << shift);
+  const int used = min(parts.n, max(1, (nkeys + parts.keys - 1) / parts.keys));
+  if (used == 1) return;   // written already
+  const float* pp = parts.partial + item * parts.n * (DH + 4);
+  float m = -INFINITY, l = 0.f, v[(DH + 63) / 64];
+  for (int s = lane; s < used; s += 64) m = fmaxf(m, pp[s * (DH + 4) + DH]);
+  m = wave_max(m);
+  const float ref = m == -INFINITY ? 0.f : m;
+#pragma unroll
+  for (int i = 0; i < (DH + 63) / 64; ++i) v[i] = 0.f;
+#pragma unroll 4
+  for (int s = 0; s < used; ++s) {
+    const float f = __builtin_amdgcn_exp2f(pp[s * (DH + 4) + DH] - ref);
+    l += pp[s * (DH + 4) + DH + 1] * f;
+#pragma unroll
+    for (int i = 0; i < (DH + 63) / 64; ++i)
+      if (DH >= 64 || lane < DH) v[i] += pp[s * (DH + 4) + lane + 64 * i] * f;
+  }
+#pragma unroll
+  for (int i = 0; i < (DH + 63) / 64; ++i)
+    if (DH >= 64 || lane < DH) o[(long)t * ldo + (long)head * DH + lane + 64 * i] = from_f<T>(l == 0.f ? 0.f : v[i] / l);
+}
+
+// Parts of the contexts, rows of a workgroup and blocks of rows
+struct Plan { int tiles, row_blocks, parts, keys; };
+Plan plan(int B, int hk, int g, int max_nodes, int max_ctx) {
+  const int rows = max_nodes * g, tiles = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
+  Plan p = {tiles, (rows + 16 * tiles - 1) / (16 * tiles), 1, 0};
+  const long groups = (long)B * hk * p.row_blocks, keys = (long)max_ctx + max_nodes;
+  long n = (2048 + groups - 1) / groups;
+  if (n > (keys + 255) / 256) n = (keys + 255) / 256;
+  p.parts = (int)(n > 1 ? n : 1);
+  return p;
+}
+
+// keys of a part, for a context of the longest length: a whole number of tiles for each wavefront
+int part_keys(long keys, int parts) { return (int)(((keys + parts - 1) / parts + 127) / 128 * 128); }
+
 }  // namespace
 
 extern "C" {
@@ -154,7 +535,9 @@ ls_status lsk_tree_index(const int32_t* parent, const int32_t* start, const int3
 }
 
 size_t lsk_attn_tree_scratch_floats(int T, int B, int h, int hk, int dh, int max_nodes, int max_ctx) {
-  return 0;
+  if (T <= 0 || B <= 0 || h <= 0 || hk <= 0 || h % hk || dh <= 0 || max_nodes <= 0 || max_ctx < 0) return 0;
+  const Plan p = plan(B, hk, h / hk, max_nodes, max_ctx);
+  return p.parts > 1 ? (size_t)T * h * p.parts * (dh + 4) : 0;
 }
 
 ls_status lsk_attn_tree(const void* q, long ldq, int dt, int T, int B, int max_nodes, int h, int hk, int dh,
@@ -173,6 +556,42 @@ ls_status lsk_attn_tree(const void* q, long ldq, int dt, int T, int B, int max_n
   const Tree tr = {start, ctx_len, mask, B, T, max_nodes, (max_nodes + 63) / 64, block_table, max_pages, page, n_pages};
   const float scale_log2 = 1.4426950408889634f / sqrtf((float)dh);
   hipStream_t st = (hipStream_t)stream;
+  if (dt != LS_F32 && (dh == 32 || dh == 64 || dh == 128) && page >= 8 && (page & (page - 1)) == 0 && ldq % 8 == 0 && ldo % 8 == 0 &&
+      ((uintptr_t)q | (uintptr_t)o | (uintptr_t)k_pool | (uintptr_t)v_pool) % 16 == 0) {
+    Plan p = plan(B, hk, h / hk, max_nodes, max_ctx);
+    const size_t one = (size_t)T * h * (dh + 4);
+    const size_t room = scratch && (uintptr_t)scratch % 16 == 0 ? scratch_floats / one : 0;
+    if ((size_t)p.parts > room) p.parts = room > 1 ? (int)room : 1;
+    const long keys = (long)max_ctx + max_nodes;
+    LS_REQUIRE(keys <= 0x7fffff00L, "attn_tree: max_ctx %d is too large", max_ctx);
+    const Parts parts = {p.parts, part_keys(keys, p.parts), p.row_blocks, scratch};
+    const long groups = ((long)B * hk + 7) / 8 * 8 * p.row_blocks;
+    LS_REQUIRE(groups <= 0x7fffffffL, "attn_tree: too many (request, head) pairs");
+    const dim3 grid((unsigned)groups, p.parts);
+    const int shift = __builtin_ctz(page);
+    auto go = [&](auto* one_, auto dh_, auto nt_) {
+      typedef std::remove_pointer_t<decltype(one_)> T_;
+      constexpr int DH = decltype(dh_)::value, NT = decltype(nt_)::value;
+      tree_attn_kernel<T_, DH, NT><<<grid, 256, 0, st>>>((const T_*)q, ldq, (T_*)o, ldo, (const T_*)k_pool, (const T_*)v_pool,
+                                                       block_table, mask, tr, h, hk, shift, scale_log2, parts);
+      if (p.parts > 1)
+        tree_merge_kernel<T_, DH><<<(unsigned)(((long)T * h + 3) / 4), 256, 0, st>>>((T_*)o, ldo, tr, h, hk, shift, parts);
+    };
+    auto rows = [&](auto* one_, auto dh_) {
+      if (p.tiles == 1) go(one_, dh_, std::integral_constant<int, 1>());
+      else if (p.tiles == 2) go(one_, dh_, std::integral_constant<int, 2>());
+      else go(one_, dh_, std::integral_constant<int, 4>());
+    };
+    auto size = [&](auto* one_) {
+      if (dh == 32) rows(one_, std::integral_constant<int, 32>());
+      else if (dh == 64) rows(one_, std::integral_constant<int, 64>());
+      else rows(one_, std::integral_constant<int, 128>());
+    };
+    if (dt == LS_BF16) size((bf16_t*)nullptr);
+    else size((f16_t*)nullptr);
+    LS_CHECK_LAUNCH();
+    return LS_OK;
+  }
   auto any = [&](auto* one) {
     typedef std::remove_pointer_t<decltype(one)> T_;
     tree_attn_any_kernel<T_><<<dim3((unsigned)T, h), 256, 0, st>>>((const T_*)q, ldq, (T_*)o, ldo, (const T_*)k_pool,

@@ -101,4 +101,6 @@ def attend(q, keys, values, seen, dtype, p_half):
     # scores: dh products and their sum, the scaling and the exponential's argument; sums over the keys in four parts or more
     ds = (dh + 8) * F32 * (np.abs(k) @ np.abs(q)).max() / np.sqrt(dh) + 8 * F32 * np.abs(s).max()
     rel = p_half + 2 * ds + (len(seen) / 4 + 80) * F32
-    return o, 1.01 * rel * mag + 1.01 * HALF[dtype] * np.abs(o) + 2.0 ** -24 * (dtype == "f16")
+    # fp16 weights below 2^-20 of the largest may be dropped: the matrix cores take subnormal operands for zero
+    dropped = 2.0 ** -20 * w.max() * np.abs(v).sum(0) if dtype == "f16" else 0.0
+    return o, 1.01 * rel * mag + 1.01 * HALF[dtype] * np.abs(o) + 2.0 ** -24 * (dtype == "f16") + dropped
