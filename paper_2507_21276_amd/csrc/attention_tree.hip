@@ -142,12 +142,15 @@ __global__ __launch_bounds__(256) void tree_attn_any_kernel(const T* q, long ldq
 
 // ---- 16-bit matrix-core kernel ------------------------------------------------------------------
 //
-// A workgroup of four wavefronts owns 16 NT rows (node, query head of one key head) of one request, one key head and one part
-// of the keys; the wavefronts share out the part's tiles of 32 keys, so that every K and V byte is loaded by one wavefront,
-// straight to registers, and serves all rows.  S^T = K Q^T (16x16x32) leaves a row's scores in one lane column; the lane's
-// eight keys of a tile are 4 q .. 4 q + 3 and 16 + 4 q .. + 3 (q = lane / 16), and O^T += V^T P^T takes P from these very
-// registers when V^T is fed in the same order of keys, which two transposing LDS reads per 16 head dimensions do.  The
-// wavefront writes its V tile to its own LDS buffer for them: no barrier in the loop.
+// A workgroup of four wavefronts owns 16 NT RW rows (node, query head of one key head) of one request, one key head and one
+// part of the keys: RW wavefronts have 16 NT rows each, and KW = 4 / RW such sets share out the part's tiles of 32 keys.
+// S^T = K Q^T (16x16x32) leaves a row's scores in one lane column; the lane's eight keys of a tile are 4 q .. 4 q + 3 and
+// 16 + 4 q .. + 3 (q = lane / 16), and O^T += V^T P^T takes P from these very registers when V^T is fed in the same order of
+// keys, which two transposing LDS reads per 16 head dimensions do.
+//   RW = 1 (up to 32 rows): bound by the K and V bytes.  Each is loaded by one wavefront; K goes straight to registers as the
+//   first product's operand, V to the wavefront's own LDS buffer: no barrier in the loop.
+//   RW = 2, 4 (more rows): bound by the exponentials and the products.  K and V tiles are loaded once for the RW wavefronts,
+//   through two LDS buffers and one barrier a tile.
 template <class T> struct Mma16;
 template <> struct Mma16<bf16_t> {
   typedef bf16x8 V8;
@@ -163,8 +166,6 @@ template <> struct Mma16<f16_t> {
 };
 
 typedef short s16x4 __attribute__((ext_vector_type(4)));
-typedef short s16x8 __attribute__((ext_vector_type(8)));
-typedef __fp16 h16x4 __attribute__((ext_vector_type(4)));
 
 // Byte offset of 16-byte piece c of row r in a V tile.  A transposing read takes 32 bytes of each of 16 rows: pairs of pieces
 // are spread over the banks by the row.
@@ -173,34 +174,44 @@ template <int DH> __device__ __forceinline__ int v_at(int r, int c) {
   const int x = DH == 128 ? r & 7 : DH == 64 ? (r >> 1) & 3 : (r >> 2) & 1;
   return r * (DH * 2) + (((c >> 1) ^ (x & (PAIRS - 1))) << 5) + ((c & 1) << 4);
 }
+// The same in a K tile, where 16 lanes read the same piece of 16 rows
+template <int DH> __device__ __forceinline__ int k_at(int r, int c) {
+  const int x = DH == 128 ? r & 15 : DH == 64 ? (r >> 1) & 7 : (r >> 2) & 3;
+  return r * (DH * 2) + ((c ^ x) << 4);
+}
 
 struct Parts {
   int n, keys;       // parts of a context, keys of each (the last takes the rest)
   int row_blocks;
-  float* partial;    // [T][h][n][dh + 2]: output, maximum (base 2), sum
+  float* partial;    // [T][h][n][dh + 4]: output, maximum (base 2), sum
 };
 
-template <class T, int DH, int NT>
-__global__ __launch_bounds__(256, NT == 4 ? 1 : 2) void tree_attn_kernel(const T* __restrict__ q, long ldq, T* __restrict__ o,
-                                                                         long ldo, const T* __restrict__ k_pool,
-                                                                         const T* __restrict__ v_pool,
-                                                                         const int32_t* __restrict__ table,
-                                                                         const uint64_t* __restrict__ masks, Tree tr, int h,
-                                                                         int hk, int shift, float scale_log2, Parts parts) {
+template <int DH, int RW> constexpr int tree_lds() {
+  constexpr int KW = 4 / RW, tile = 32 * DH * 2, work = RW == 1 ? 4 * tile : 2 * KW * 2 * tile, join = 4 * 16 * (DH + 4) * 4;
+  return work > join ? work : join;
+}
+
+template <class T, int DH, int NT, int RW>
+__global__ __launch_bounds__(256, 2) void tree_attn_kernel(const T* __restrict__ q, long ldq, T* __restrict__ o, long ldo,
+                                                           const T* __restrict__ k_pool, const T* __restrict__ v_pool,
+                                                           const int32_t* __restrict__ table,
+                                                           const uint64_t* __restrict__ masks, Tree tr, int h, int hk,
+                                                           int shift, float scale_log2, Parts parts) {
   typedef typename Mma16<T>::V8 V8;
-  constexpr int KS = DH / 32, DT = DH / 16, NL = DH / 16, LPR = DH / 8;   // loads of K, and of V, per tile; lanes per V row
-  constexpr int TILE = 32 * DH * 2, WAVE_LDS = TILE > 2048 * NT ? TILE : 2048 * NT;
-  constexpr int JOIN = 4 * 16 * (DH + 4) * 4;
-  __shared__ __attribute__((aligned(16))) char smem[4 * WAVE_LDS > JOIN ? 4 * WAVE_LDS : JOIN];
+  constexpr int KW = 4 / RW, ROWS = 16 * NT * RW;
+  constexpr int KS = DH / 32, DT = DH / 16, LPR = DH / 8;   // steps of the first product, of the second; lanes per row loaded
+  constexpr int NL = DH / 16 / RW;                          // loads of K, and of V, per wavefront and tile
+  constexpr int TILE = 32 * DH * 2;
+  __shared__ __attribute__((aligned(16))) char smem[tree_lds<DH, RW>()];
   __shared__ float s_m[4][NT * 16], s_l[4][NT * 16];
+  __shared__ int s_odd[2][KW];
 
   // Blocks of rows that read the same keys follow each other on one XCD (workgroups go round the eight of them)
   const int slot8 = blockIdx.x >> 3, item = (slot8 / parts.row_blocks) * 8 + (blockIdx.x & 7), rb = slot8 % parts.row_blocks;
   if (item >= tr.B * hk) return;
   const int b = item / hk, kvh = item % hk, part = blockIdx.y, g = h / hk;
   const int first = tr.start[b], nodes = min(min(tr.start[b + 1], tr.T) - first, tr.max_nodes), rows = nodes * g;
-  const int row0 = rb * (16 * NT);
-  if (first < 0 || row0 >= rows) return;
+  if (first < 0 || rb * ROWS >= rows) return;
   const int ctx = max(tr.ctx_len[b], 0), page = 1 << shift;
   const int nkeys = (int)min((long)ctx + nodes, (long)tr.max_pages * page);
   const int used = min(parts.n, max(1, (nkeys + parts.keys - 1) / parts.keys));   // parts of this request
@@ -208,16 +219,16 @@ __global__ __launch_bounds__(256, NT == 4 ? 1 : 2) void tree_attn_kernel(const T
   const int k_lo = part * parts.keys, k_hi = part == used - 1 ? nkeys : k_lo + parts.keys;
   const int t_lo = k_lo / 32, t_hi = (k_hi + 31) / 32;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, col = lane & 15, quad = lane >> 4;
+  const int rw = wave % RW, kw = wave / RW, row0 = rb * ROWS + rw * 16 * NT;
   const int32_t* bt = table + (long)b * tr.max_pages;
-  char* vt = smem + wave * WAVE_LDS;
 
   V8 qf[NT][KS];
-  int node[NT];      // of the lane's row
+  int node[NT];      // of the lane's row; rows past the last repeat it
 #pragma unroll
   for (int n = 0; n < NT; ++n) {
-    const int r = row0 + n * 16 + col;
-    node[n] = min(r, rows - 1) / g;
-    const T* qr = q + (long)(first + node[n]) * ldq + (long)(kvh * g + (r < rows ? r % g : g - 1)) * DH;
+    const int r = min(row0 + n * 16 + col, rows - 1);
+    node[n] = r / g;
+    const T* qr = q + (long)(first + node[n]) * ldq + (long)(kvh * g + r % g) * DH;
 #pragma unroll
     for (int s = 0; s < KS; ++s) qf[n][s] = *(const V8*)(qr + s * 32 + quad * 8);
   }
@@ -244,33 +255,46 @@ __global__ __launch_bounds__(256, NT == 4 ? 1 : 2) void tree_attn_kernel(const T
       w.at[i] = ((((long)id * hk + kvh) << shift) + (key & (page - 1))) * DH;
     }
   };
-  auto fetch = [&](const Where& w, V8 (&kf)[NL], V8 (&vf)[NL]) {
-    const int hi8 = (lane >> 3) & 1;
+  V8 kf[RW == 1 ? 2 * KS : NL], vf[NL];
+  // row and piece of load j of this wavefront in whole-row order, and where its row group lies
+  auto row_of = [&](int j) { return (rw * NL + j) * (64 / LPR) + lane / LPR; };
+  auto group_at = [&](const Where& w, int j) {
+    const long a0 = w.at[0], a1 = w.at[1], a2 = w.at[2], a3 = w.at[3];
+    const int i = row_of(j) >> 3;
+    return i < 2 ? (i == 0 ? a0 : a1) : (i == 2 ? a2 : a3);
+  };
+  auto fetch_k = [&](const Where& w) {
+    if constexpr (RW == 1) {   // the lane's operand of the first product
 #pragma unroll
-    for (int c = 0; c < 2; ++c) {
-      const T* kr = k_pool + (hi8 ? w.at[2 * c + 1] : w.at[2 * c]) + (lane & 7) * DH + quad * 8;
+      for (int c = 0; c < 2; ++c) {
+        const long a0 = w.at[2 * c], a1 = w.at[2 * c + 1];
+        const T* kr = k_pool + ((lane >> 3) & 1 ? a1 : a0) + (lane & 7) * DH + quad * 8;
 #pragma unroll
-      for (int s = 0; s < KS; ++s) kf[c * KS + s] = *(const V8*)(kr + s * 32);
-    }
+        for (int s = 0; s < KS; ++s) kf[c * KS + s] = *(const V8*)(kr + s * 32);
+      }
+    } else {
 #pragma unroll
-    for (int j = 0; j < NL; ++j) {
-      const int r = j * (64 / LPR) + lane / LPR;
-      const long at = DH == 128 ? w.at[j >> 1] : DH == 64 ? w.at[j & 3] : (lane >> 5) ? w.at[(2 * j + 1) & 3] : w.at[(2 * j) & 3];
-      vf[j] = *(const V8*)(v_pool + at + (r & 7) * DH + (lane % LPR) * 8);
+      for (int j = 0; j < NL; ++j)
+        kf[j] = *(const V8*)(k_pool + group_at(w, j) + (row_of(j) & 7) * DH + (lane % LPR) * 8);
     }
   };
-  auto attend = [&](int t, const V8 (&kf)[NL], const V8 (&vf)[NL], int bad) {
-    const int k0 = t * 32;
-    const bool plain = k0 + 32 <= ctx && k0 + 32 <= k_hi && bad == 0;   // all rows see all keys
-    // V to LDS.  In the tiles that some row does not see whole, values that are not finite are left out of the product (0 * x
-    // would reach the rows that do not see them) and added to the rows that do afterwards.
+  auto fetch_v = [&](const Where& w) {
+#pragma unroll
+    for (int j = 0; j < NL; ++j)
+      vf[j] = *(const V8*)(v_pool + group_at(w, j) + (row_of(j) & 7) * DH + (lane % LPR) * 8);
+  };
+  auto is_plain = [&](int t, int bad) { return t * 32 + 32 <= ctx && t * 32 + 32 <= k_hi && bad == 0; };   // all rows see all keys
+  // V to LDS.  In the tiles that some row does not see whole, values that are not finite are left out of the product (0 * x
+  // would reach the rows that do not see them); returns whether there were any.
+  auto put_v = [&](char* vt, int t, int bad) {
     bool odd = false;
+    const bool plain = is_plain(t, bad);
 #pragma unroll
     for (int j = 0; j < NL; ++j) {
-      const int r = j * (64 / LPR) + lane / LPR;
+      const int r = row_of(j);
       u32x4 v = __builtin_bit_cast(u32x4, vf[j]);
       if (!plain) {
-        const bool live = k0 + r < k_hi && !(bad >> (r >> 3) & 1);
+        const bool live = t * 32 + r < k_hi && !(bad >> (r >> 3) & 1);
         constexpr uint32_t E = Mma16<T>::kExp;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
@@ -281,15 +305,28 @@ __global__ __launch_bounds__(256, NT == 4 ? 1 : 2) void tree_attn_kernel(const T
       }
       *(u32x4*)(vt + v_at<DH>(r, lane % LPR)) = v;
     }
-    f32x4 sacc[NT][2];
+    return __builtin_amdgcn_ballot_w64(odd) != 0;
+  };
+
+  f32x4 sacc[NT][2];
+  auto first_product = [&](const char* kt) {
 #pragma unroll
-    for (int n = 0; n < NT; ++n)
+    for (int n = 0; n < NT; ++n) sacc[n][0] = sacc[n][1] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int c = 0; c < 2; ++c) {
-        sacc[n][c] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int c = 0; c < 2; ++c)
 #pragma unroll
-        for (int s = 0; s < KS; ++s) sacc[n][c] = Mma16<T>::run(kf[c * KS + s], qf[n][s], sacc[n][c]);
+      for (int s = 0; s < KS; ++s) {
+        V8 ka;
+        if constexpr (RW == 1) ka = kf[c * KS + s];
+        else ka = *(const V8*)(kt + k_at<DH>(16 * c + col, 4 * s + quad));
+#pragma unroll
+        for (int n = 0; n < NT; ++n) sacc[n][c] = Mma16<T>::run(ka, qf[n][s], sacc[n][c]);
       }
+  };
+  // softmax and second product of tile t from the scores in sacc
+  auto attend = [&](const char* vt, int t, int bad, bool odd) {
+    const int k0 = t * 32;
+    const bool plain = is_plain(t, bad);
     uint32_t seen[NT];   // bit r: the lane's row sees key k0 + r
     if (!plain) {
       uint32_t live = k_hi - k0 >= 32 ? ~0u : (1u << (k_hi - k0)) - 1;
@@ -350,35 +387,28 @@ __global__ __launch_bounds__(256, NT == 4 ? 1 : 2) void tree_attn_kernel(const T
       // keys 4 quad + (col / 4), head dimensions 16 j + 4 (col % 4) ..: the lane receives its column of the 4 x 16 block
       const char* p0 = vt + v_at<DH>(4 * quad + (col >> 2), 2 * j + ((col >> 1) & 1)) + (col & 1) * 8;
       const char* p1 = vt + v_at<DH>(16 + 4 * quad + (col >> 2), 2 * j + ((col >> 1) & 1)) + (col & 1) * 8;
-      const s16x4 lo = __builtin_bit_cast(s16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                           (__attribute__((address_space(3))) s16x4*)p0));
-      const s16x4 hi = __builtin_bit_cast(s16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                           (__attribute__((address_space(3))) s16x4*)p1));
+      const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)p0);
+      const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)p1);
       const V8 vfrag = __builtin_bit_cast(V8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
 #pragma unroll
       for (int n = 0; n < NT; ++n) oacc[n][j] = Mma16<T>::run(vfrag, pf[n], oacc[n][j]);
     }
-    if (!plain && __builtin_amdgcn_ballot_w64(odd) != 0) {
-      // Rare: a value of this tile is infinite or NaN.  The weights go to LDS (-1: not seen), then key by key the values that
-      // were left out are read again and added where they are seen.
-      float* ps = (float*)vt;
+    if (!plain && odd) {
+      // Rare: values of this tile are infinite or NaN.  Key by key, what was left out is read again and added where it is seen.
       Where w;
       find(t, w);
-#pragma unroll
-      for (int n = 0; n < NT; ++n)
-#pragma unroll
-        for (int c = 0; c < 2; ++c)
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-            ps[((16 * c + 4 * quad + i) * NT + n) * 16 + col] = seen[n] >> (16 * c + 4 * quad + i) & 1 ? sacc[n][c][i] : -1.f;
 #pragma unroll 1
       for (int r = 0; r < 32; ++r) {
         if (k0 + r >= k_hi || (bad >> (r >> 3) & 1)) continue;
-        const long at = r < 8 ? w.at[0] : r < 16 ? w.at[1] : r < 24 ? w.at[2] : w.at[3];
-        const T* vr = v_pool + at + (r & 7) * DH;
-        float p[NT];
+        const long a0 = w.at[0], a1 = w.at[1], a2 = w.at[2], a3 = w.at[3];
+        const T* vr = v_pool + (r < 16 ? (r < 8 ? a0 : a1) : (r < 24 ? a2 : a3)) + (r & 7) * DH;
+        float p[NT];   // the weight of key r in the lane's row: held by the lane of that row and the key's quad
 #pragma unroll
-        for (int n = 0; n < NT; ++n) p[n] = ps[(r * NT + n) * 16 + col];
+        for (int n = 0; n < NT; ++n) {
+          const f32x4 half = r < 16 ? sacc[n][0] : sacc[n][1];
+          const float x = (r & 2) ? ((r & 1) ? half[3] : half[2]) : ((r & 1) ? half[1] : half[0]);
+          p[n] = __shfl(x, ((r >> 2) & 3) * 16 + col, 64);
+        }
 #pragma unroll
         for (int j = 0; j < DT; ++j)
 #pragma unroll
@@ -387,39 +417,69 @@ __global__ __launch_bounds__(256, NT == 4 ? 1 : 2) void tree_attn_kernel(const T
             if (v - v != 0.f) {
 #pragma unroll
               for (int n = 0; n < NT; ++n)
-                if (p[n] >= 0.f || p[n] != p[n]) oacc[n][j][i] += p[n] * v;
+                if (seen[n] >> r & 1) oacc[n][j][i] += p[n] * v;
             }
           }
       }
     }
   };
 
-  int t = t_lo + wave;
-  if (t < t_hi) {
-    Where w0, w1;
-    V8 k0[NL], v0[NL], k1[NL], v1[NL];
-    find(t, w0);
-    fetch(w0, k0, v0);
-    int bad0 = w0.bad, bad1 = 0;
-    if (t + 4 < t_hi) find(t + 4, w1);
-    for (; t < t_hi; t += 8) {
-      if (t + 4 < t_hi) {
-        fetch(w1, k1, v1);
-        bad1 = w1.bad;
-        if (t + 8 < t_hi) find(t + 8, w0);
+  if constexpr (RW == 1) {
+    // The next tile's V is asked for as soon as this one's is in LDS, its K after the first product: a wavefront nearly
+    // always has a tile in flight
+    char* vt = smem + wave * TILE;
+    int t = t_lo + wave;
+    if (t < t_hi) {
+      Where next;
+      find(t, next);
+      fetch_v(next);
+      fetch_k(next);
+      for (; t < t_hi; t += 4) {
+        const int bad = next.bad;
+        const bool more = t + 4 < t_hi;
+        if (more) find(t + 4, next);
+        const bool odd = put_v(vt, t, bad);
+        if (more) fetch_v(next);
+        first_product(nullptr);
+        if (more) fetch_k(next);
+        attend(vt, t, bad, odd);
       }
-      attend(t, k0, v0, bad0);
-      if (t + 4 < t_hi) {
-        if (t + 8 < t_hi) {
-          fetch(w0, k0, v0);
-          bad0 = w0.bad;
-          if (t + 12 < t_hi) find(t + 12, w1);
-        }
-        attend(t + 4, k1, v1, bad1);
+    }
+  } else {
+    if (threadIdx.x < 2 * KW) s_odd[threadIdx.x / KW][threadIdx.x % KW] = -1;
+    __syncthreads();
+    Where next;
+    int t = t_lo + kw;
+    if (t < t_hi) {
+      find(t, next);
+      fetch_v(next);
+      fetch_k(next);
+    }
+    for (int i = t_lo; i < t_hi; i += KW, t += KW) {   // the same number of trips in every wavefront
+      const int buf = (i - t_lo) / KW & 1, bad = next.bad;
+      char* kt = smem + (buf * KW + kw) * 2 * TILE;
+      char* vt = kt + TILE;
+      if (t < t_hi) {
+        if (put_v(vt, t, bad)) s_odd[buf][kw] = t;
+#pragma unroll
+        for (int j = 0; j < NL; ++j) *(V8*)(kt + k_at<DH>(row_of(j), lane % LPR)) = kf[j];
+      }
+      if (t + KW < t_hi) {
+        find(t + KW, next);
+        fetch_v(next);
+        fetch_k(next);
+      }
+      // all are past the tile before this one: its buffer is the next to be written
+      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+      __builtin_amdgcn_s_barrier();
+      __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+      if (t < t_hi) {
+        first_product(kt);
+        attend(vt, t, bad, s_odd[buf][kw] == t);
       }
     }
   }
-  // Join the four wavefronts, 16 rows at a time, through LDS
+  // Join the KW sets, 16 rows of each wavefront at a time, through LDS
 #pragma unroll
   for (int n = 0; n < NT; ++n) {
     float l = l_run[n] + __shfl_xor(l_run[n], 16, 64);
@@ -427,46 +487,45 @@ __global__ __launch_bounds__(256, NT == 4 ? 1 : 2) void tree_attn_kernel(const T
     if (quad == 0) { s_m[wave][n * 16 + col] = m_run[n]; s_l[wave][n * 16 + col] = l; }
   }
   float* so = (float*)smem;   // [wave][row][DH + 4]
+  constexpr int TPR = 16 / RW;   // threads a row
+  const int r = threadIdx.x / TPR, jw = r >> 4, jr = r & 15;
 #pragma unroll
   for (int n = 0; n < NT; ++n) {
     __syncthreads();
 #pragma unroll
     for (int j = 0; j < DT; ++j) *(f32x4*)(so + (wave * 16 + col) * (DH + 4) + 16 * j + 4 * quad) = oacc[n][j];
     __syncthreads();
-    const int r = threadIdx.x >> 4, row = row0 + n * 16 + r;   // 16 threads a row
+    const int row = rb * ROWS + (jw * NT + n) * 16 + jr;
     if (row < rows) {
-      const float mm = fmaxf(fmaxf(s_m[0][n * 16 + r], s_m[1][n * 16 + r]), fmaxf(s_m[2][n * 16 + r], s_m[3][n * 16 + r]));
-      const float ref = mm == -INFINITY ? 0.f : mm;
-      float f[4], l = 0.f;
+      float mm = -INFINITY, f[KW], l = 0.f;
 #pragma unroll
-      for (int w = 0; w < 4; ++w) {
-        f[w] = __builtin_amdgcn_exp2f(s_m[w][n * 16 + r] - ref);
-        l += s_l[w][n * 16 + r] * f[w];
+      for (int w = 0; w < KW; ++w) mm = fmaxf(mm, s_m[w * RW + jw][n * 16 + jr]);
+      const float ref = mm == -INFINITY ? 0.f : mm;
+#pragma unroll
+      for (int w = 0; w < KW; ++w) {
+        f[w] = __builtin_amdgcn_exp2f(s_m[w * RW + jw][n * 16 + jr] - ref);   // a set without a tile: weight 0 and zeros
+        l += s_l[w * RW + jw][n * 16 + jr] * f[w];
       }
       const long trow = first + row / g, head = kvh * g + row % g;
-      const float inv = l == 0.f ? 0.f : 1.f / l;   // a row that sees nothing: zeros
-      for (int c = (threadIdx.x & 15) * 4; c < DH; c += 64) {
+      const float inv = 1.f / l;
+      float* pp = parts.partial + ((trow * h + head) * parts.n + part) * (DH + 4);
+      for (int c = (threadIdx.x % TPR) * 4; c < DH; c += 4 * TPR) {
         f32x4 v = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int w = 0; w < 4; ++w) {
-          const f32x4 x = *(const f32x4*)(so + (w * 16 + r) * (DH + 4) + c);
-          // a wavefront without a tile has weight 0 and zeros
-          v += x * f[w];
-        }
+        for (int w = 0; w < KW; ++w) v += *(const f32x4*)(so + ((w * RW + jw) * 16 + jr) * (DH + 4) + c) * f[w];
         if (used == 1) {
           typedef T V4 __attribute__((ext_vector_type(4)));
           V4 out;
 #pragma unroll
-          for (int i = 0; i < 4; ++i) out[i] = from_f<T>(l == 0.f ? 0.f : v[i] * inv);
+          for (int i = 0; i < 4; ++i) out[i] = from_f<T>(l == 0.f ? 0.f : v[i] * inv);   // a row that sees nothing: zeros
           *(V4*)(o + trow * ldo + head * DH + c) = out;
         } else {
-          *(f32x4*)(parts.partial + ((trow * h + head) * parts.n + part) * (DH + 4) + c) = v;
+          *(f32x4*)(pp + c) = v;
         }
       }
-      if (used > 1 && (threadIdx.x & 15) == 0) {
-        float* pp = parts.partial + ((trow * h + head) * parts.n + part) * (DH + 4) + DH;
-        pp[0] = mm;
-        pp[1] = l;
+      if (used > 1 && threadIdx.x % TPR == 0) {
+        pp[DH] = mm;
+        pp[DH + 1] = l;
       }
     }
   }
@@ -504,11 +563,12 @@ __global__ __launch_bounds__(256) void tree_merge_kernel(T* __restrict__ o, long
     if (DH >= 64 || lane < DH) o[(long)t * ldo + (long)head * DH + lane + 64 * i] = from_f<T>(l == 0.f ? 0.f : v[i] / l);
 }
 
-// Parts of the contexts, rows of a workgroup and blocks of rows
-struct Plan { int tiles, row_blocks, parts, keys; };
-Plan plan(int B, int hk, int g, int max_nodes, int max_ctx) {
-  const int rows = max_nodes * g, tiles = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
-  Plan p = {tiles, (rows + 16 * tiles - 1) / (16 * tiles), 1, 0};
+// Rows of a workgroup (tiles of 16 a wavefront, wavefronts with rows of their own), blocks of rows, parts of the contexts
+struct Plan { int tiles, row_waves, row_blocks, parts; };
+Plan plan(int B, int hk, int g, int dh, int max_nodes, int max_ctx) {
+  // head_dim 32: a tile is two loads, for two wavefronts
+  const int rows = max_nodes * g, tiles = rows <= 16 ? 1 : 2, row_waves = rows <= 32 ? 1 : rows <= 64 || dh == 32 ? 2 : 4;
+  Plan p = {tiles, row_waves, (rows + 16 * tiles * row_waves - 1) / (16 * tiles * row_waves), 1};
   const long groups = (long)B * hk * p.row_blocks, keys = (long)max_ctx + max_nodes;
   long n = (2048 + groups - 1) / groups;
   if (n > (keys + 255) / 256) n = (keys + 255) / 256;
@@ -536,7 +596,7 @@ ls_status lsk_tree_index(const int32_t* parent, const int32_t* start, const int3
 
 size_t lsk_attn_tree_scratch_floats(int T, int B, int h, int hk, int dh, int max_nodes, int max_ctx) {
   if (T <= 0 || B <= 0 || h <= 0 || hk <= 0 || h % hk || dh <= 0 || max_nodes <= 0 || max_ctx < 0) return 0;
-  const Plan p = plan(B, hk, h / hk, max_nodes, max_ctx);
+  const Plan p = plan(B, hk, h / hk, dh, max_nodes, max_ctx);
   return p.parts > 1 ? (size_t)T * h * p.parts * (dh + 4) : 0;
 }
 
@@ -558,7 +618,7 @@ ls_status lsk_attn_tree(const void* q, long ldq, int dt, int T, int B, int max_n
   hipStream_t st = (hipStream_t)stream;
   if (dt != LS_F32 && (dh == 32 || dh == 64 || dh == 128) && page >= 8 && (page & (page - 1)) == 0 && ldq % 8 == 0 && ldo % 8 == 0 &&
       ((uintptr_t)q | (uintptr_t)o | (uintptr_t)k_pool | (uintptr_t)v_pool) % 16 == 0) {
-    Plan p = plan(B, hk, h / hk, max_nodes, max_ctx);
+    Plan p = plan(B, hk, h / hk, dh, max_nodes, max_ctx);
     const size_t one = (size_t)T * h * (dh + 4);
     const size_t room = scratch && (uintptr_t)scratch % 16 == 0 ? scratch_floats / one : 0;
     if ((size_t)p.parts > room) p.parts = room > 1 ? (int)room : 1;
@@ -569,18 +629,23 @@ ls_status lsk_attn_tree(const void* q, long ldq, int dt, int T, int B, int max_n
     LS_REQUIRE(groups <= 0x7fffffffL, "attn_tree: too many (request, head) pairs");
     const dim3 grid((unsigned)groups, p.parts);
     const int shift = __builtin_ctz(page);
-    auto go = [&](auto* one_, auto dh_, auto nt_) {
+    auto go = [&](auto* one_, auto dh_, auto nt_, auto rw_) {
       typedef std::remove_pointer_t<decltype(one_)> T_;
-      constexpr int DH = decltype(dh_)::value, NT = decltype(nt_)::value;
-      tree_attn_kernel<T_, DH, NT><<<grid, 256, 0, st>>>((const T_*)q, ldq, (T_*)o, ldo, (const T_*)k_pool, (const T_*)v_pool,
-                                                       block_table, mask, tr, h, hk, shift, scale_log2, parts);
+      constexpr int DH = decltype(dh_)::value, NT = decltype(nt_)::value, RW = decltype(rw_)::value;
+      tree_attn_kernel<T_, DH, NT, RW><<<grid, 256, 0, st>>>((const T_*)q, ldq, (T_*)o, ldo, (const T_*)k_pool,
+                                                           (const T_*)v_pool, block_table, mask, tr, h, hk, shift, scale_log2,
+                                                           parts);
       if (p.parts > 1)
         tree_merge_kernel<T_, DH><<<(unsigned)(((long)T * h + 3) / 4), 256, 0, st>>>((T_*)o, ldo, tr, h, hk, shift, parts);
     };
     auto rows = [&](auto* one_, auto dh_) {
-      if (p.tiles == 1) go(one_, dh_, std::integral_constant<int, 1>());
-      else if (p.tiles == 2) go(one_, dh_, std::integral_constant<int, 2>());
-      else go(one_, dh_, std::integral_constant<int, 4>());
+      const std::integral_constant<int, 1> c1;
+      const std::integral_constant<int, 2> c2;
+      const std::integral_constant<int, 4> c4;
+      if (p.tiles == 1) go(one_, dh_, c1, c1);
+      else if (p.row_waves == 1) go(one_, dh_, c2, c1);
+      else if (p.row_waves == 2) go(one_, dh_, c2, c2);
+      else if constexpr (decltype(dh_)::value > 32) go(one_, dh_, c2, c4);
     };
     auto size = [&](auto* one_) {
       if (dh == 32) rows(one_, std::integral_constant<int, 32>());
