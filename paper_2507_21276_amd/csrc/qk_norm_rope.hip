@@ -6,6 +6,9 @@
 //   dg = sum over rows and heads of du * x r,   dx = r (g du - x r^2 S / dh),   S = sum(g du x).
 #include <math.h>
 
+#include <initializer_list>
+#include <type_traits>
+
 #include "common.h"
 
 namespace {
@@ -179,20 +182,261 @@ __global__ __launch_bounds__(256) void norm_rope_bwd_any_kernel(const void* dout
     partial[((size_t)part * gridDim.x + blockIdx.x) * s.dh + c] = s_dg[0][c] + s_dg[1][c] + s_dg[2][c] + s_dg[3][c];
 }
 
-// dgain (+)= alpha * sum over the workgroups, in their order; 64 columns of one part a workgroup, 16 wavefronts
+// ---- vectorised kernels: dh <= 256 and rot multiples of 8, rows and bases aligned to four elements ----------------------
+//
+// LPH lanes have a head, each eight of its elements: four pairs, in two vectors of four.  Pairs are local to a lane in
+// either layout, and r takes one sum over the lanes, in lane permutations without LDS.  A lane keeps the angles of its
+// row and the gains, which are as many bytes as a head itself, over the heads that it works through.
+// Bound by the bytes of the rows.
+
+template <int LPH> __device__ __forceinline__ float head_sum(float v) {
+  v = dpp_add<0xb1, 0xf>(v);                  // lane ^ 1
+  v = dpp_add<0x4e, 0xf>(v);                  // lane ^ 2
+  if (LPH >= 8) v = dpp_add<0x141, 0xf>(v);   // mirrored in eight
+  if (LPH >= 16) v = dpp_add<0x140, 0xf>(v);  // mirrored in sixteen
+  if (LPH >= 32) v += __shfl_xor(v, 16, 64);
+  return v;
+}
+
+template <class T> struct Four { typedef T type __attribute__((ext_vector_type(4))); };
+
+// A lane's place in a head: its two vectors, and what it keeps of its row
+template <class T, int LAYOUT> struct Lane {
+  typedef typename Four<T>::type V4;
+  int oa, ob;
+  bool live, turned;
+  float c[4], s[4];
+  __device__ __forceinline__ Lane(const Shape& sh, int sub) {
+    live = 8 * sub < sh.dh;
+    turned = 8 * sub < sh.rot;
+    oa = LAYOUT == 0 && turned ? 4 * sub : 8 * sub;
+    ob = LAYOUT == 0 && turned ? 4 * sub + sh.rot / 2 : 8 * sub + 4;
+  }
+  __device__ __forceinline__ void row(const Shape& sh, int sub, int t) {
+    if (!turned) return;
+    const f32x4* cs = (const f32x4*)(angles(sh, t) + 8 * sub);
+    const f32x4 x = cs[0], y = cs[1];
+    c[0] = x[0]; s[0] = x[1]; c[1] = x[2]; s[1] = x[3];
+    c[2] = y[0]; s[2] = y[1]; c[3] = y[2]; s[3] = y[3];
+  }
+  // element e < 4 of vector a or b of pair p: the half layout has the pair (a[p], b[p]), neighbours are (v[2p], v[2p + 1])
+  __device__ __forceinline__ void turn(float (&a)[4], float (&b)[4], float sign) const {
+    if (!turned) return;
+    if (LAYOUT == 0) {
+#pragma unroll
+      for (int p = 0; p < 4; ++p) {
+        const float sn = sign * s[p], x = a[p] * c[p] - b[p] * sn;
+        b[p] = a[p] * sn + b[p] * c[p];
+        a[p] = x;
+      }
+    } else {
+#pragma unroll
+      for (int p = 0; p < 4; ++p) {
+        float& u = p < 2 ? a[2 * p] : b[2 * p - 4];
+        float& w = p < 2 ? a[2 * p + 1] : b[2 * p - 3];
+        const float sn = sign * s[p], x = u * c[p] - w * sn;
+        w = u * sn + w * c[p];
+        u = x;
+      }
+    }
+  }
+};
+
+__device__ __forceinline__ void load_gain(const void* gain, int pdt, int oa, int ob, bool live, float (&g)[8]) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e) g[e] = gain && live ? load_as_f(gain, (e < 4 ? oa : ob) + (e & 3), pdt) : 1.f;
+}
+
+constexpr int kHeads = 4;   // heads of a lane in flight
+
+// `per` groups of lanes share a token's heads (a power of two); blockIdx.y takes kHeads of each group
+template <class T, int LAYOUT, int LPH, int MODE>
+__global__ __launch_bounds__(256) void norm_rope_kernel(const T* in, long ld_in, T* out, long ld_out, Shape s, Pages pg, int per) {
+  typedef typename Four<T>::type V4;
+  const int sub = threadIdx.x % LPH, grp = threadIdx.x / LPH;
+  const long t = (long)blockIdx.x * (256 / LPH / per) + grp / per;
+  if (t >= s.T) return;
+  const int heads = s.h + s.hk + (MODE == IN_PLACE ? 0 : s.hk), first = grp % per + blockIdx.y * per * kHeads;
+  if (first >= heads) return;
+  Lane<T, LAYOUT> ln(s, sub);
+  long at = 0;
+  if (MODE == TO_PAGES) {
+    if (pg.req[t] < 0) return;
+    at = slot_of(pg, (int)t, s.hk, s.dh);
+  }
+  const T* src = in + t * ld_in;
+  V4 a[kHeads], b[kHeads];
+#pragma unroll
+  for (int u = 0; u < kHeads; ++u) {
+    const int hd = first + u * per;
+    a[u] = b[u] = V4{};
+    if (hd < heads && ln.live) {
+      a[u] = *(const V4*)(src + (long)hd * s.dh + ln.oa);
+      b[u] = *(const V4*)(src + (long)hd * s.dh + ln.ob);
+    }
+  }
+  if (s.rot) ln.row(s, sub, (int)t);
+  float gq[8], gk[8];
+  load_gain(s.gain_q, s.pdt, ln.oa, ln.ob, ln.live, gq);
+  load_gain(s.gain_k, s.pdt, ln.oa, ln.ob, ln.live, gk);
+#pragma unroll
+  for (int u = 0; u < kHeads; ++u) {
+    const int hd = first + u * per;
+    if (hd >= heads) break;
+    const int part = hd < s.h ? 0 : hd < s.h + s.hk ? 1 : 2;
+    float x[4], y[4], sq = 0.f;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      x[e] = to_f(a[u][e]);
+      y[e] = to_f(b[u][e]);
+      sq += x[e] * x[e] + y[e] * y[e];
+    }
+    if (part < 2) {
+      const float r = s.norm ? rsqrtf(head_sum<LPH>(sq) / s.dh + s.eps) : 1.f;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        x[e] = x[e] * r * (part == 0 ? gq[e] : gk[e]);
+        y[e] = y[e] * r * (part == 0 ? gq[e + 4] : gk[e + 4]);
+      }
+      ln.turn(x, y, 1.f);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) { a[u][e] = from_f<T>(x[e]); b[u][e] = from_f<T>(y[e]); }
+    }
+    if (!ln.live) continue;
+    T* dst = out + t * ld_out + (long)hd * s.dh;
+    if (MODE == TO_PAGES && part > 0) {
+      if (at < 0) continue;
+      dst = (T*)(part == 1 ? pg.k_pool : pg.v_pool) + at + (long)(hd - s.h - (part - 1) * s.hk) * pg.page * s.dh;
+    }
+    *(V4*)(dst + ln.oa) = a[u];
+    *(V4*)(dst + ln.ob) = b[u];
+  }
+}
+
+// Backward: a workgroup walks tokens, its lanes keep the gains' gradients of their elements and the workgroup's sum goes to
+// partial[part][blockIdx.x][dh].
+template <class T, int LAYOUT, int LPH>
+__global__ __launch_bounds__(256) void norm_rope_bwd_kernel(const T* dout, long ld_dout, const T* in, long ld_in, T* din,
+                                                            long ld_din, Shape s, int per, int copy_v, float* partial) {
+  typedef typename Four<T>::type V4;
+  __shared__ float s_dg[256 * 8];
+  constexpr int U = 2;
+  const int sub = threadIdx.x % LPH, grp = threadIdx.x / LPH, tokens = 256 / LPH / per, g0 = grp % per;
+  Lane<T, LAYOUT> ln(s, sub);
+  float gain[2][8], dg[2][8];
+  load_gain(s.gain_q, s.pdt, ln.oa, ln.ob, ln.live, gain[0]);
+  load_gain(s.gain_k, s.pdt, ln.oa, ln.ob, ln.live, gain[1]);
+#pragma unroll
+  for (int e = 0; e < 8; ++e) dg[0][e] = dg[1][e] = 0.f;
+  for (long t = (long)blockIdx.x * tokens + grp / per; t < s.T; t += (long)gridDim.x * tokens) {
+    if (s.rot) ln.row(s, sub, (int)t);
+    const T *dy = dout + t * ld_dout, *xr = in + t * ld_in;
+    T* dx = din + t * ld_din;
+#pragma unroll
+    for (int part = 0; part < 2; ++part) {
+      const int lo = part == 0 ? 0 : s.h, n = part == 0 ? s.h : s.hk;
+      for (int h0 = g0; h0 < n; h0 += per * U) {
+        V4 da[U], db[U], xa[U], xb[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          const int hd = h0 + u * per;
+          const long at = (long)(lo + hd) * s.dh;
+          da[u] = db[u] = xa[u] = xb[u] = V4{};
+          if (hd < n && ln.live) {
+            da[u] = *(const V4*)(dy + at + ln.oa);
+            db[u] = *(const V4*)(dy + at + ln.ob);
+            if (s.norm) {
+              xa[u] = *(const V4*)(xr + at + ln.oa);
+              xb[u] = *(const V4*)(xr + at + ln.ob);
+            }
+          }
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          const int hd = h0 + u * per;
+          if (hd >= n) break;
+          float w[4], z[4], sq = 0.f, dot = 0.f;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) { w[e] = to_f(da[u][e]); z[e] = to_f(db[u][e]); }
+          ln.turn(w, z, -1.f);
+          if (s.norm) {
+            float x[4], y[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              x[e] = to_f(xa[u][e]);
+              y[e] = to_f(xb[u][e]);
+              sq += x[e] * x[e] + y[e] * y[e];
+              dot += w[e] * gain[part][e] * x[e] + z[e] * gain[part][e + 4] * y[e];
+            }
+            const float r = rsqrtf(head_sum<LPH>(sq) / s.dh + s.eps), back = head_sum<LPH>(dot) * r * r / s.dh;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              dg[part][e] += w[e] * x[e] * r;
+              dg[part][e + 4] += z[e] * y[e] * r;
+              w[e] = r * (w[e] * gain[part][e] - x[e] * back);
+              z[e] = r * (z[e] * gain[part][e + 4] - y[e] * back);
+            }
+          }
+          if (!ln.live) continue;
+          const long at = (long)(lo + hd) * s.dh;
+          V4 oa, ob;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) { oa[e] = from_f<T>(w[e]); ob[e] = from_f<T>(z[e]); }
+          *(V4*)(dx + at + ln.oa) = oa;
+          *(V4*)(dx + at + ln.ob) = ob;
+        }
+      }
+    }
+    if (copy_v && ln.live)
+      for (int hd = g0; hd < s.hk; hd += per) {
+        const long at = (long)(s.h + s.hk + hd) * s.dh;
+        const V4 va = *(const V4*)(dy + at + ln.oa), vb = *(const V4*)(dy + at + ln.ob);
+        *(V4*)(dx + at + ln.oa) = va;
+        *(V4*)(dx + at + ln.ob) = vb;
+      }
+  }
+  if (!partial) return;
+#pragma unroll
+  for (int part = 0; part < 2; ++part) {
+    __syncthreads();
+    if (ln.live) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) s_dg[grp * (LPH * 8) + (e < 4 ? ln.oa + e : ln.ob + e - 4)] = dg[part][e];
+    }
+    __syncthreads();
+    for (int c = threadIdx.x; c < s.dh; c += 256) {
+      float v = 0.f;
+      for (int g = 0; g < 256 / LPH; ++g) v += s_dg[g * (LPH * 8) + c];
+      partial[((size_t)part * gridDim.x + blockIdx.x) * s.dh + c] = v;
+    }
+  }
+}
+
+// dgain (+)= alpha * sum over the workgroups, in a fixed order; 16 columns of one part a workgroup, 64 rows at a time
 __global__ __launch_bounds__(1024) void gain_sum_kernel(const float* partial, int blocks, int dh, float* dgq, float* dgk,
                                                         int accumulate, const float* alpha) {
-  __shared__ float s_sum[16][64];
-  const int part = blockIdx.y, wave = threadIdx.x >> 6, lane = threadIdx.x & 63, c = blockIdx.x * 64 + lane;
+  __shared__ float s_sum[64][17];
+  const int part = blockIdx.y, row = threadIdx.x >> 4, lane = threadIdx.x & 15, c = blockIdx.x * 16 + lane;
+  const float* src = partial + (size_t)part * blocks * dh + c;
   float v = 0.f;
-  if (c < dh)
-    for (int b = wave; b < blocks; b += 16) v += partial[((size_t)part * blocks + b) * dh + c];
-  s_sum[wave][lane] = v;
+  if (c < dh) {
+    int b = row;
+    for (; b + 192 < blocks; b += 256) {   // four loads in flight
+      const float v0 = src[(size_t)b * dh], v1 = src[(size_t)(b + 64) * dh], v2 = src[(size_t)(b + 128) * dh],
+                  v3 = src[(size_t)(b + 192) * dh];
+      v += (v0 + v1) + (v2 + v3);
+    }
+    for (; b < blocks; b += 64) v += src[(size_t)b * dh];
+  }
+  s_sum[row][lane] = v;
   __syncthreads();
-  if (wave > 0 || c >= dh) return;
+  if (threadIdx.x >= 64) return;
   v = 0.f;
 #pragma unroll
-  for (int w = 0; w < 16; ++w) v += s_sum[w][lane];
+  for (int i = 0; i < 16; ++i) v += s_sum[(threadIdx.x >> 4) * 16 + i][lane];
+  v += __shfl_xor(v, 16, 64);
+  v += __shfl_xor(v, 32, 64);
+  if (threadIdx.x >= 16 || c >= dh) return;
   if (alpha) v *= alpha[0];
   float* out = part == 0 ? dgq : dgk;
   out[c] = accumulate ? out[c] + v : v;
@@ -233,6 +477,7 @@ __global__ __launch_bounds__(256) void rope_table_kernel(float* table, int n_pos
 ls_status check_shape(const char* who, int dt, const Shape& s, int layout) {
   LS_REQUIRE(dt == LS_F32 || dt == LS_BF16 || dt == LS_F16, "%s: unknown dtype %d", who, dt);
   LS_REQUIRE(s.T > 0 && s.h > 0 && s.hk > 0, "%s: non-positive size (T %d, heads %d, %d)", who, s.T, s.h, s.hk);
+  LS_REQUIRE(s.h <= 65535, "%s: %d heads, at most 65535", who, s.h);
   LS_REQUIRE(s.h % s.hk == 0, "%s: %d query heads do not share %d key heads evenly", who, s.h, s.hk);
   LS_REQUIRE(s.dh >= 2 && s.dh <= 512 && s.dh % 2 == 0, "%s: head_dim %d is not even or outside 2..512", who, s.dh);
   LS_REQUIRE((long)s.T * (s.h + 2L * s.hk) <= 0x7fffffffL * 4, "%s: too many (row, head) pairs", who);
@@ -251,13 +496,60 @@ Shape make_shape(int T, int h, int hk, int dh, int kind, const void* gq, const v
   return Shape{T, h, hk, dh, rot, kind, eps, gq, gk, pdt, pos, table, max_pos};
 }
 
+// Which shapes the vectorised kernels take, and the lanes of a head
+bool vec_covers(int dt, const Shape& s, std::initializer_list<const void*> rows, std::initializer_list<long> lds) {
+  const size_t bytes = 4 * dtype_size(dt);
+  for (const void* p : rows)
+    if ((uintptr_t)p % bytes) return false;
+  for (const long ld : lds)
+    if (ld % 4) return false;
+  return s.dh % 8 == 0 && s.dh <= 256 && s.rot % 8 == 0 && (s.rot == 0 || (uintptr_t)s.table % 16 == 0);
+}
+
+int pow2_from(int n) {
+  int p = 1;
+  while (p < n) p *= 2;
+  return p;
+}
+
+// f(type tag, layout, lanes of a head) for the shape's instance
+template <class F> void vec_instance(int dt, int layout, int dh, F f) {
+  auto lanes = [&](auto one, auto lay) {
+    switch (pow2_from(dh / 8)) {
+      case 32: f(one, lay, std::integral_constant<int, 32>()); break;
+      case 16: f(one, lay, std::integral_constant<int, 16>()); break;
+      case 8: f(one, lay, std::integral_constant<int, 8>()); break;
+      default: f(one, lay, std::integral_constant<int, 4>());   // smaller heads leave lanes over
+    }
+  };
+  auto type = [&](auto lay) {
+    if (dt == LS_F32) lanes((float*)nullptr, lay);
+    else if (dt == LS_BF16) lanes((bf16_t*)nullptr, lay);
+    else lanes((f16_t*)nullptr, lay);
+  };
+  if (layout == LSK_ROPE_HALF) type(std::integral_constant<int, 0>());
+  else type(std::integral_constant<int, 1>());
+}
+
 template <int MODE>
 ls_status launch_fwd(const void* in, long ld_in, void* out, long ld_out, int dt, Shape s, int layout, const Pages& pg,
                      hipStream_t st) {
   s.norm = s.norm == 1;
-  const long items = (long)s.T * (s.h + s.hk + (MODE == IN_PLACE ? 0 : s.hk));
+  const int heads = s.h + s.hk + (MODE == IN_PLACE ? 0 : s.hk);
+  if (vec_covers(dt, s, {in, out, pg.k_pool, pg.v_pool}, {ld_in, ld_out})) {
+    vec_instance(dt, layout, s.dh, [&](auto* one, auto lay, auto lph) {
+      typedef std::remove_pointer_t<decltype(one)> T;
+      constexpr int LPH = decltype(lph)::value, groups = 256 / LPH;
+      const int need = pow2_from(heads), per = need < groups ? need : groups, tokens = groups / per;
+      const dim3 grid((unsigned)((s.T + tokens - 1) / tokens), (heads + per * kHeads - 1) / (per * kHeads));
+      norm_rope_kernel<T, decltype(lay)::value, LPH, MODE><<<grid, 256, 0, st>>>((const T*)in, ld_in, (T*)out, ld_out, s, pg, per);
+    });
+    LS_CHECK_LAUNCH();
+    return LS_OK;
+  }
+  const long items = (long)s.T * heads;
   const unsigned grid = (unsigned)((items + 3) / 4);
-  if (layout == 0) norm_rope_any_kernel<0, MODE><<<grid, 256, 0, st>>>(in, ld_in, out, ld_out, dt, s, pg);
+  if (layout == LSK_ROPE_HALF) norm_rope_any_kernel<0, MODE><<<grid, 256, 0, st>>>(in, ld_in, out, ld_out, dt, s, pg);
   else norm_rope_any_kernel<1, MODE><<<grid, 256, 0, st>>>(in, ld_in, out, ld_out, dt, s, pg);
   LS_CHECK_LAUNCH();
   return LS_OK;
@@ -355,14 +647,26 @@ ls_status lsk_qk_norm_rope_bwd(const void* dout, long ld_dout, const void* in, l
   LS_REQUIRE(!dgain_q || partial, "qk_norm_rope_bwd: null partial");
   hipStream_t st = (hipStream_t)stream;
   s.norm = s.norm == 1;
-  const int blocks = bwd_blocks((long)T * h);
+  int blocks = bwd_blocks((long)T * h);
   float* sums = dgain_q ? partial : nullptr;
-  const dim3 grid(blocks, din == dout ? 2 : 3);
-  if (layout == 0) norm_rope_bwd_any_kernel<0><<<grid, 256, 0, st>>>(dout, ld_dout, in, ld_in, din, ld_din, dt, s, sums);
-  else norm_rope_bwd_any_kernel<1><<<grid, 256, 0, st>>>(dout, ld_dout, in, ld_in, din, ld_din, dt, s, sums);
+  if (vec_covers(dt, s, {dout, s.norm ? in : nullptr, din}, {ld_dout, s.norm ? ld_in : 0, ld_din})) {
+    vec_instance(dt, layout, dh, [&](auto* one, auto lay, auto lph) {
+      typedef std::remove_pointer_t<decltype(one)> T_;
+      constexpr int LPH = decltype(lph)::value, groups = 256 / LPH;
+      const int need = pow2_from(h), per = need < groups ? need : groups, tokens = groups / per;
+      const long all = ((long)T + tokens - 1) / tokens;
+      if (all < blocks) blocks = (int)all;
+      norm_rope_bwd_kernel<T_, decltype(lay)::value, LPH><<<blocks, 256, 0, st>>>(
+          (const T_*)dout, ld_dout, (const T_*)in, ld_in, (T_*)din, ld_din, s, per, din != dout, sums);
+    });
+  } else {
+    const dim3 grid(blocks, din == dout ? 2 : 3);
+    if (layout == LSK_ROPE_HALF) norm_rope_bwd_any_kernel<0><<<grid, 256, 0, st>>>(dout, ld_dout, in, ld_in, din, ld_din, dt, s, sums);
+    else norm_rope_bwd_any_kernel<1><<<grid, 256, 0, st>>>(dout, ld_dout, in, ld_in, din, ld_din, dt, s, sums);
+  }
   LS_CHECK_LAUNCH();
   if (sums) {
-    gain_sum_kernel<<<dim3((dh + 63) / 64, 2), 1024, 0, st>>>(sums, blocks, dh, dgain_q, dgain_k, accumulate, alpha_dev);
+    gain_sum_kernel<<<dim3((dh + 15) / 16, 2), 1024, 0, st>>>(sums, blocks, dh, dgain_q, dgain_k, accumulate, alpha_dev);
     LS_CHECK_LAUNCH();
   }
   return LS_OK;
