@@ -598,111 +598,148 @@ def lsk_finish_qkv(partial, splits, n_heads, head_dim, pos, req, table, qkv, k_p
 
 
 # ---- the cache path of drafted tokens ------------------------------------------------------------
+#
+# These calls are small next to a projection: what the host does per call is kept short, and each shape is looked at once.
 
-def _rows(t):
-    """Pointer and row distance of a matrix whose rows are dense."""
-    assert t.dim() == 2 and (t.shape[1] == 1 or t.stride(1) == 1), "rows must be dense"
-    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else t.shape[1]
+_INT = torch.int32
 
 
-def _norm_rope(head_dim, gain_q, gain_k, norm, eps, pos, table, layout):
+def _here(t, stream):
+    """The stream of a call on t: t's device has to be the current one, and its current stream is the default."""
+    dev = t.get_device()
+    assert dev == torch._C._cuda_getDevice(), "tensors on another device than the current one"
+    return torch._C._cuda_getCurrentRawStream(dev) if stream is None else _stream(stream)
+
+
+def _at(t):
+    """Pointer of a dense tensor, None for none."""
+    if t is None:
+        return None
+    assert t.is_contiguous()
+    return t.data_ptr()
+
+
+def _rows(t, T, width):
+    """Pointer and row distance of a matrix of T rows of at least width elements, dense within a row."""
+    (n, w), (ld, one) = t.shape, t.stride()
+    assert n == T and w >= width and (one == 1 or w == 1), "rows must be dense and wide enough"
+    return t.data_ptr(), ld if n > 1 else w
+
+
+def _indexes(t, n):
+    """Pointer of at least n 32-bit integers, None for none."""
+    if t is None:
+        return None
+    assert t.dtype is _INT and t.numel() >= n and t.is_contiguous(), "dense 32-bit integers, one a row"
+    return t.data_ptr()
+
+
+def _norm_rope(T, head_dim, gain_q, gain_k, norm, eps, pos, table, layout):
     """The arguments that the forms of lsk_qk_norm_rope share, from kind on."""
     gain = gain_q if gain_q is not None else gain_k
-    assert gain_q is None or gain_q.numel() == head_dim
-    assert gain_k is None or (gain_k.numel() == head_dim and gain_k.dtype == gain.dtype)
-    assert table is None or (table.dtype == torch.float32 and pos is not None and pos.dtype == torch.int32)
-    return (1 if norm else -1, _opt(gain_q), _opt(gain_k), CODE_OF_TORCH[gain.dtype] if gain is not None else 0, eps,
-            2 * table.shape[1] if table is not None else 0, layout, _opt(pos), _opt(table),
-            table.shape[0] if table is not None else 0)
+    code = 0
+    if gain is not None:
+        code = CODE_OF_TORCH[gain.dtype]
+        assert gain.numel() == head_dim and (gain_k is None or (gain_k.numel() == head_dim and gain_k.dtype is gain.dtype))
+    rot = n_pos = 0
+    if table is not None:
+        n_pos, half, two = table.shape
+        rot = 2 * half
+        assert two == 2 and table.dtype is torch.float32 and pos is not None, "an fp32 table of cos and sin needs positions"
+    return 1 if norm else -1, _at(gain_q), _at(gain_k), code, eps, rot, layout, _indexes(pos, T), _at(table), n_pos
 
 
 def lsk_rope_table(table, theta, scaling=None, stream=None):
     """Fills table [n_pos, rot_dim / 2, 2] with cos and sin."""
-    assert table.dtype == torch.float32 and table.dim() == 3 and table.shape[2] == 2
-    _check(lib().lsk_rope_table(_p(table), table.shape[0], 2 * table.shape[1], theta,
-                                C.byref(scaling) if scaling is not None else None, _stream(stream)))
+    n_pos, half, two = table.shape
+    assert two == 2 and table.dtype is torch.float32
+    _check(lib().lsk_rope_table(_at(table), n_pos, 2 * half, theta, scaling, _here(table, stream)))
 
 
 def lsk_qk_norm_rope(qkv, out, n_heads, n_kv_heads, head_dim, *, gain_q=None, gain_k=None, norm=True, eps=1e-5, pos=None,
                      table=None, layout=LSK_ROPE_HALF, stream=None):
     """out = norm and rotation of q and k, and v, of qkv [T, (n_heads + 2 n_kv_heads) head_dim]; table [.., rot_dim / 2, 2]."""
-    assert qkv.shape == out.shape and qkv.dtype == out.dtype and qkv.shape[1] == (n_heads + 2 * n_kv_heads) * head_dim
-    assert pos is None or pos.numel() >= qkv.shape[0]
-    _check(lib().lsk_qk_norm_rope(*_rows(qkv), *_rows(out), CODE_OF_TORCH[qkv.dtype], qkv.shape[0], n_heads, n_kv_heads, head_dim,
-                                  *_norm_rope(head_dim, gain_q, gain_k, norm, eps, pos, table, layout), _stream(stream)))
+    T, width = qkv.shape[0], (n_heads + 2 * n_kv_heads) * head_dim
+    assert qkv.dtype is out.dtype
+    _check(lib().lsk_qk_norm_rope(*_rows(qkv, T, width), *_rows(out, T, width), CODE_OF_TORCH[qkv.dtype], T, n_heads, n_kv_heads,
+                                  head_dim, *_norm_rope(T, head_dim, gain_q, gain_k, norm, eps, pos, table, layout),
+                                  _here(qkv, stream)))
 
 
 def lsk_qk_norm_rope_bwd(dout, qkv, din, n_heads, n_kv_heads, head_dim, *, gain_q=None, gain_k=None, norm=True, eps=1e-5,
                          pos=None, table=None, layout=LSK_ROPE_HALF, dgain_q=None, dgain_k=None, accumulate=False, alpha=None,
                          stream=None):
     """din from dout and the forward's input; dgain_q, dgain_k (fp32, both or neither) (+)= alpha * the gains' gradients."""
-    assert dout.shape == din.shape and dout.dtype == din.dtype and dout.shape[1] == (n_heads + 2 * n_kv_heads) * head_dim
-    assert qkv is None or (qkv.shape == dout.shape and qkv.dtype == dout.dtype)
-    assert pos is None or pos.numel() >= dout.shape[0]
-    T, partial = dout.shape[0], None
-    for g in (dgain_q, dgain_k):
-        assert g is None or (g.dtype == torch.float32 and g.numel() == head_dim)
+    T, width, L, partial = dout.shape[0], (n_heads + 2 * n_kv_heads) * head_dim, lib(), None
+    assert dout.dtype is din.dtype and (qkv is None or qkv.dtype is dout.dtype)
     if dgain_q is not None:
-        n = lib().lsk_qk_norm_rope_bwd_partial_floats(T, n_heads, n_kv_heads, head_dim)
-        partial = torch.empty(n, dtype=torch.float32, device=dout.device)
-    _check(lib().lsk_qk_norm_rope_bwd(*_rows(dout), *(_rows(qkv) if qkv is not None else (None, 0)), *_rows(din),
-                                      CODE_OF_TORCH[dout.dtype], T, n_heads, n_kv_heads, head_dim,
-                                      *_norm_rope(head_dim, gain_q, gain_k, norm, eps, pos, table, layout), _opt(dgain_q),
-                                      _opt(dgain_k), int(accumulate), _opt(alpha), _opt(partial), _stream(stream)))
+        assert dgain_k is not None and dgain_q.dtype is dgain_k.dtype is torch.float32, "both gradients of the gains, in fp32"
+        assert dgain_q.numel() == head_dim == dgain_k.numel()
+        partial = torch.empty(L.lsk_qk_norm_rope_bwd_partial_floats(T, n_heads, n_kv_heads, head_dim), dtype=torch.float32,
+                              device=dout.device)
+    _check(L.lsk_qk_norm_rope_bwd(*_rows(dout, T, width), *(_rows(qkv, T, width) if qkv is not None else (None, 0)),
+                                  *_rows(din, T, width), CODE_OF_TORCH[dout.dtype], T, n_heads, n_kv_heads, head_dim,
+                                  *_norm_rope(T, head_dim, gain_q, gain_k, norm, eps, pos, table, layout), _at(dgain_q), _at(dgain_k),
+                                  1 if accumulate else 0, _at(alpha), _at(partial), _here(dout, stream)))
+
+
+def _pools(k_pool, v_pool, n_kv_heads, page_size, head_dim, dtype):
+    """Pointers of the pools and the number of their pages."""
+    shape = k_pool.shape
+    assert shape == v_pool.shape and shape[1:] == (n_kv_heads, page_size, head_dim) and k_pool.dtype is v_pool.dtype is dtype
+    return _at(k_pool), _at(v_pool), shape[0]
 
 
 def lsk_qk_norm_rope_kv_write(qkv, q_out, n_heads, n_kv_heads, head_dim, pos, req, k_pool, v_pool, block_table, page_size, *,
                               slot=None, gain_q=None, gain_k=None, norm=True, eps=1e-5, table=None, layout=LSK_ROPE_HALF,
                               stream=None):
     """q of qkv, normalised and rotated, to q_out; k and v to their slots of the pools [n_pages, n_kv_heads, page, head_dim]."""
-    T = qkv.shape[0]
-    assert qkv.dtype == q_out.dtype == k_pool.dtype == v_pool.dtype and qkv.shape[1] == (n_heads + 2 * n_kv_heads) * head_dim
-    assert q_out.shape[0] == T and q_out.shape[1] >= n_heads * head_dim
-    assert k_pool.shape == v_pool.shape and tuple(k_pool.shape[1:]) == (n_kv_heads, page_size, head_dim)
-    assert req.numel() >= T and all(t is None or t.numel() >= T for t in (pos, slot))
-    _check(lib().lsk_qk_norm_rope_kv_write(*_rows(qkv), *_rows(q_out), CODE_OF_TORCH[qkv.dtype], T, n_heads, n_kv_heads, head_dim,
-                                           *_norm_rope(head_dim, gain_q, gain_k, norm, eps, pos, table, layout), _p(req),
-                                           _opt(slot), _p(k_pool), _p(v_pool), _p(block_table), block_table.shape[1], page_size,
-                                           k_pool.shape[0], _stream(stream)))
+    T, dtype = qkv.shape[0], qkv.dtype
+    assert q_out.dtype is dtype and block_table.dtype is _INT
+    kp, vp, n_pages = _pools(k_pool, v_pool, n_kv_heads, page_size, head_dim, dtype)
+    _check(lib().lsk_qk_norm_rope_kv_write(*_rows(qkv, T, (n_heads + 2 * n_kv_heads) * head_dim), *_rows(q_out, T, n_heads * head_dim),
+                                           CODE_OF_TORCH[dtype], T, n_heads, n_kv_heads, head_dim,
+                                           *_norm_rope(T, head_dim, gain_q, gain_k, norm, eps, pos, table, layout),
+                                           _indexes(req, T), _indexes(slot, T), kp, vp, _at(block_table), block_table.shape[1],
+                                           page_size, n_pages, _here(qkv, stream)))
 
 
 def lsk_tree_index(parent, start, ctx_len, max_nodes, pos, slot, req, mask, stream=None):
     """pos, slot, req [T] and mask [T, ceil(max_nodes / 64)] (64-bit words) of the trees that parent [T] and start [B + 1] give."""
-    T = pos.numel()
-    assert parent.numel() >= T and slot.numel() >= T and req.numel() >= T and mask.shape == (T, (max_nodes + 63) // 64)
-    assert mask.element_size() == 8 and all(t.dtype == torch.int32 for t in (parent, start, ctx_len, pos, slot, req))
-    _check(lib().lsk_tree_index(_p(parent), _p(start), _p(ctx_len), start.numel() - 1, T, max_nodes, _p(pos), _p(slot), _p(req),
-                                _p(mask), _stream(stream)))
+    T, B = pos.numel(), start.numel() - 1
+    assert mask.shape == (T, (max_nodes + 63) // 64) and mask.element_size() == 8
+    _check(lib().lsk_tree_index(_indexes(parent, T), _indexes(start, 2), _indexes(ctx_len, B), B, T, max_nodes, _indexes(pos, T),
+                                _indexes(slot, T), _indexes(req, T), _at(mask), _here(pos, stream)))
 
 
 def lsk_attn_tree(q, o, n_heads, n_kv_heads, head_dim, start, ctx_len, mask, max_nodes, k_pool, v_pool, block_table, page_size,
                   max_ctx, scratch=None, stream=None):
     """o [T, n_heads head_dim] of the drafted trees' rows q over the pools [n_pages, n_kv_heads, page, head_dim]."""
-    T, B = q.shape[0], start.numel() - 1
-    assert q.dtype == o.dtype == k_pool.dtype == v_pool.dtype and o.shape[0] == T and mask.shape == (T, (max_nodes + 63) // 64)
-    assert q.shape[1] >= n_heads * head_dim and o.shape[1] >= n_heads * head_dim and mask.element_size() == 8
-    assert k_pool.shape == v_pool.shape and tuple(k_pool.shape[1:]) == (n_kv_heads, page_size, head_dim)
+    T, B, dtype, L = q.shape[0], start.numel() - 1, q.dtype, lib()
+    assert o.dtype is dtype and mask.shape == (T, (max_nodes + 63) // 64) and mask.element_size() == 8 and block_table.dtype is _INT
+    kp, vp, n_pages = _pools(k_pool, v_pool, n_kv_heads, page_size, head_dim, dtype)
     if scratch is None:
-        n = lib().lsk_attn_tree_scratch_floats(T, B, n_heads, n_kv_heads, head_dim, max_nodes, max_ctx)
-        scratch = torch.empty(n, dtype=torch.float32, device=q.device) if n else None
-    _check(lib().lsk_attn_tree(*_rows(q), CODE_OF_TORCH[q.dtype], T, B, max_nodes, n_heads, n_kv_heads, head_dim, _p(start),
-                               _p(ctx_len), _p(mask), _p(k_pool), _p(v_pool), _p(block_table), block_table.shape[1], page_size,
-                               k_pool.shape[0], max_ctx, *_rows(o), _opt(scratch),
-                               scratch.numel() if scratch is not None else 0, _stream(stream)))
+        n = L.lsk_attn_tree_scratch_floats(T, B, n_heads, n_kv_heads, head_dim, max_nodes, max_ctx)
+        if n:
+            scratch = torch.empty(n, dtype=torch.float32, device=q.device)
+    else:
+        n = scratch.numel()
+        assert scratch.dtype is torch.float32
+    _check(L.lsk_attn_tree(*_rows(q, T, n_heads * head_dim), CODE_OF_TORCH[dtype], T, B, max_nodes, n_heads, n_kv_heads, head_dim,
+                           _indexes(start, 2), _indexes(ctx_len, B), _at(mask), kp, vp, _at(block_table), block_table.shape[1],
+                           page_size, n_pages, max_ctx, *_rows(o, T, n_heads * head_dim), _at(scratch), n, _here(q, stream)))
 
 
 def lsk_kv_copy_pages(config, kv, src, dst, stream=None):
     """Pages src[i] -> dst[i] (host integers) of all layers; config: the pool's ls_config."""
     n = len(src)
     assert len(dst) == n
-    d = kv.desc(False)
-    a, b = (C.c_int32 * max(1, n))(*src), (C.c_int32 * max(1, n))(*dst)
-    _check(lib().lsk_kv_copy_pages(C.byref(config), C.byref(d), a, b, n, _stream(stream)))
+    ints = C.c_int32 * (n or 1)
+    _check(lib().lsk_kv_copy_pages(config, kv.desc(False), ints(*src), ints(*dst), n, _here(kv.k_pool, stream)))
 
 
 def lsk_kv_move_rows(config, kv, path, n_path, stream=None):
     """Rows of the accepted nodes path [B, max_path] (n_path [B] of them) of every request to the end of its context."""
-    assert path.dtype == n_path.dtype == torch.int32 and n_path.numel() == path.shape[0]
-    d = kv.desc(False)
-    _check(lib().lsk_kv_move_rows(C.byref(config), C.byref(d), path.shape[0], _p(path), path.shape[1], _p(n_path),
-                                  _stream(stream)))
+    B, most = path.shape
+    _check(lib().lsk_kv_move_rows(config, kv.desc(False), B, _indexes(path, B * most), most, _indexes(n_path, B),
+                                  _here(path, stream)))
