@@ -91,6 +91,34 @@ ls_status ls_server_pass(ls_server* sv, double now, void* workspace, void* strea
 /* Requests waiting for admission plus requests in the batch. */
 int ls_server_in_flight(const ls_server* sv);
 
+/*
+ * Books over the pages of a pool for a program that runs its own serving loop (stage_decode, stage_verify): which pages each
+ * row of the block table holds, how many rows hold a page, and which are free.  Host memory only, allocated in
+ * ls_pages_create; device copies that a call asks for are the caller's to enqueue (lsk_kv_copy_pages), after earlier work on
+ * the pages and before later one.  One owner thread.
+ *
+ * ls_pages_row      the page ids of a row, max_pages_per_row of them (0 past the last), and their number; either may be null.
+ * ls_pages_grow     gives a row pages for n_tokens tokens, of which written_from .. n_tokens - 1 are about to be written: pages
+ *                   of these that other rows hold too are replaced by free ones.  Where such a page also holds tokens before
+ *                   written_from, its copy is asked for in src / dst (capacity max_pages_per_row, at most one in fact).  A row
+ *                   that is long enough already keeps its length.  LS_ENOMEM, and nothing changed, without enough free pages.
+ * ls_pages_fork     gives row `to`, which has no pages, the pages of the first n_tokens tokens of row `from`: nothing is copied
+ *                   until one of the two grows into a shared page.
+ * ls_pages_truncate returns the pages past n_tokens tokens (0: all of them; a rejected draft, a finished request); a page is
+ *                   free once no row holds it.
+ * ls_pages_compact  packs the used pages into the lowest ids, so that the pool's end can be given up; src / dst (capacity
+ *                   n_pages) receive the moves, *n_moves their number.  No page is both read and written.
+ */
+typedef struct ls_pages ls_pages; /* opaque */
+ls_status ls_pages_create(int n_pages, int page_size, int max_rows, int max_pages_per_row, ls_pages** out);
+void ls_pages_destroy(ls_pages* p);
+int ls_pages_available(const ls_pages* p);
+ls_status ls_pages_row(const ls_pages* p, int row, int32_t* ids, int* n);
+ls_status ls_pages_grow(ls_pages* p, int row, int written_from, int n_tokens, int32_t* src, int32_t* dst, int* n_copies);
+ls_status ls_pages_fork(ls_pages* p, int from, int to, int n_tokens);
+ls_status ls_pages_truncate(ls_pages* p, int row, int n_tokens);
+ls_status ls_pages_compact(ls_pages* p, int32_t* src, int32_t* dst, int* n_moves);
+
 #ifdef __cplusplus
 }
 #endif

@@ -206,6 +206,21 @@ ls_status stage_step(ls_stage* s, const void* X, int n_decode, const int32_t* ch
                      int n_prefill, const ls_kv* kv, void* Y, void* workspace, void* stream);
 
 /*
+ * Verification of drafted tokens (speculative decoding): one forward over a tree of drafted continuations of every request.
+ * Request b contributes n_nodes[b] rows of X, 1 .. 256, the nodes of its tree; a node's parent comes before it, and a root
+ * continues the context.  Node i at depth d sits at position ctx_len[b] + d and sees the request's cached tokens, its
+ * ancestors and itself: its row of Y is what stage_decode would give after its ancestors (up to rounding order).
+ *   X, Y [dev] [T, d] io_dtype, T = sum of n_nodes;  n_nodes [host] [B], B <= 65535;
+ *   start [dev] [B+1] int32: first row of each request, start[B] = T (the sums of n_nodes);
+ *   parent [dev] [T] int32: parent's index in the request's tree, -1 for a root (see lsk_tree_index).
+ * K and V of node i are written to slot ctx_len[b] + i.  Accepting a path: lsk_kv_move_rows, then the caller advances
+ * ctx_len[b] by its length; the other nodes' rows lie beyond the context again.  The workspace is one of T tokens
+ * (ls_workspace_bytes).  LS_EINVAL as stage_prefill, with ctx_len[b] + n_nodes[b] tokens.
+ */
+ls_status stage_verify(ls_stage* s, const void* X, const int32_t* parent, const int32_t* start, const int32_t* n_nodes, int B,
+                       const ls_kv* kv, void* Y, void* workspace, void* stream);
+
+/*
  * Model update after training tasks (Model Update Synchronization: every
  * co-located instance applies its own local updates, and the inference tasks
  * that follow on the same stage are served from the updated weights).  The

@@ -82,6 +82,7 @@ SIGNATURES = {
     "stage_prefill": (_I, [_VP, _VP, C.POINTER(C.c_int32), _I, C.POINTER(ls_kv), _VP, _VP, _VP]),
     "stage_decode": (_I, [_VP, _VP, _I, C.POINTER(ls_kv), _VP, _VP, _VP]),
     "stage_step": (_I, [_VP, _VP, _I, C.POINTER(C.c_int32), _I, C.POINTER(ls_kv), _VP, _VP, _VP]),
+    "stage_verify": (_I, [_VP, _VP, _VP, _VP, C.POINTER(C.c_int32), _I, C.POINTER(ls_kv), _VP, _VP, _VP]),
     "stage_train_fwd": (_I, [_VP, _VP, _I, _I, _VP, _VP, _VP, _VP]),
     "stage_train_bwd": (_I, [_VP, _VP, _I, _I, _VP, _VP, _VP, _I, _VP, _VP]),
     "stage_probe_interference": (_I, [_VP, _VP, _I, C.POINTER(ls_kv), _VP, _VP, _VP, _I, _I, _VP, _VP,
@@ -177,6 +178,14 @@ SIGNATURES = {
     "ls_server_submit": (_I, [_VP, C.c_int64, _VP, _VP, _I, _I]),
     "ls_server_pass": (_I, [_VP, _D, _VP, _VP, _VP, C.POINTER(C.c_int64), C.POINTER(C.c_int64)]),
     "ls_server_in_flight": (_I, [_VP]),
+    "ls_pages_create": (_I, [_I, _I, _I, _I, C.POINTER(_VP)]),
+    "ls_pages_destroy": (None, [_VP]),
+    "ls_pages_available": (_I, [_VP]),
+    "ls_pages_row": (_I, [_VP, _I, C.POINTER(C.c_int32), C.POINTER(_I)]),
+    "ls_pages_grow": (_I, [_VP, _I, _I, _I, C.POINTER(C.c_int32), C.POINTER(C.c_int32), C.POINTER(_I)]),
+    "ls_pages_fork": (_I, [_VP, _I, _I, _I]),
+    "ls_pages_truncate": (_I, [_VP, _I, _I]),
+    "ls_pages_compact": (_I, [_VP, C.POINTER(C.c_int32), C.POINTER(C.c_int32), C.POINTER(_I)]),
 }
 
 
@@ -318,6 +327,12 @@ class Stage:
     def stage_decode(self, X, B, kv: KV, Y, workspace, stream=None, with_host=True):
         d = kv.desc(with_host)
         _check(lib().stage_decode(self.h, _p(X), B, C.byref(d), _p(Y), _p(workspace), _stream(stream)))
+
+    def stage_verify(self, X, parent, start, n_nodes, kv: KV, Y, workspace, stream=None, with_host=True):
+        n = (C.c_int32 * max(1, len(n_nodes)))(*[int(v) for v in n_nodes])
+        d = kv.desc(with_host)
+        _check(lib().stage_verify(self.h, _p(X), _p(parent), _p(start), n, len(n_nodes), C.byref(d), _p(Y), _p(workspace),
+                                  _stream(stream)))
 
     def stage_train_fwd(self, X, B, L, Y, saved, workspace, stream=None):
         _check(lib().stage_train_fwd(self.h, _p(X), B, L, _p(Y), _p(saved), _p(workspace), _stream(stream)))

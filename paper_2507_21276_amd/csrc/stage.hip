@@ -289,10 +289,12 @@ size_t carve_saved(const ls_stage* s, void* base, int T, std::vector<Saved>* out
 
 // forward / serving scratch
 struct FwdWs {
-  int32_t *pos, *req;
+  int32_t *pos, *req, *slot;
+  uint64_t* mask;
   float *xa, *xb, *scratch;
   void *h, *qkv, *o, *up, *act;
 };
+constexpr int kMaxNodes = 256;   // of a drafted tree: four words of its mask
 // fp32 scratch for split decode attention and split-K decode GEMMs (both are
 // only used for small row counts, where these bounds hold)
 size_t serve_scratch_floats(const ls_stage* s) {
@@ -317,6 +319,8 @@ size_t carve_fwd(const ls_stage* s, void* base, int T, FwdWs* w) {
   v.up = b.take((size_t)T * s->up_cols * e);
   v.act = b.take((size_t)T * c.d_ff * e);
   v.scratch = (float*)b.take(serve_scratch_floats(s) * 4);
+  v.slot = (int32_t*)b.take((size_t)T * 4);
+  v.mask = (uint64_t*)b.take((size_t)T * (kMaxNodes / 64) * 8);
   if (w) *w = v;
   return b.used;
 }
@@ -429,13 +433,35 @@ ls_status serve_attention(const ls_stage* s, int T, const FwdBufs& f, const int3
                         attn_scratch(s, T, max_ctx, f.scratch), st);
 }
 
+// Drafted trees of a verification (null elsewhere): rows of request b from start[b] on, node slots and masks
+struct Drafts {
+  const int32_t *start, *slot;
+  const uint64_t* mask;
+  int max_nodes, max_past;
+};
+
+// rotary embedding, page write and attention of a verification, from the projected rows in f.qkv
+ls_status verify_attention(const ls_stage* s, int T, const FwdBufs& f, const int32_t* pos, const int32_t* req, int B,
+                           const ls_kv* kv, void* kp, void* vp, const Drafts& dr, hipStream_t st) {
+  const ls_config& c = s->cfg;
+  const int d = c.d_model, mt = c.mma_dtype, h = c.n_heads, dh = c.head_dim;
+  const bool gpt = c.block == LS_BLOCK_GPT_PRELN;
+  LS_TRY(lsk_qk_norm_rope_kv_write(f.qkv, 3L * d, f.qkv, 3L * d, mt, T, h, h, dh, -1, nullptr, nullptr, c.dtype, c.norm_eps,
+                                   gpt ? 0 : dh, LSK_ROPE_HALF, pos, s->rope_table, c.max_pos, req, dr.slot, kp, vp,
+                                   kv->block_table, kv->max_pages_per_req, c.page_size, kv->n_pages, st));
+  return lsk_attn_tree(f.qkv, 3L * d, mt, T, B, dr.max_nodes, h, h, dh, dr.start, kv->ctx_len, dr.mask, kp, vp, kv->block_table,
+                       kv->max_pages_per_req, c.page_size, kv->n_pages, dr.max_past, f.o, d, f.scratch,
+                       f.scratch ? serve_scratch_floats(s) : 0, st);
+}
+
 // n_decode (serving with chunk_start only): the first n_decode rows are single-token decode rows of
 // requests 0 .. n_decode - 1; chunk_start then describes requests n_decode .. B - 1 (rows after them)
 // h1_ready (serving calls only, else null): on entry, whether the previous block's last kernel has already
 // written this block's normalised input to f.h1; on return, whether this block has done so for the next one.
 ls_status block_forward(const ls_stage* s, int l, int T, const FwdBufs& f, const int32_t* pos,
                         const int32_t* req, int B, int L, const ls_kv* kv, int max_ctx,
-                        const int32_t* chunk_start, int n_decode, hipStream_t st, bool* h1_ready = nullptr) {
+                        const int32_t* chunk_start, int n_decode, hipStream_t st, bool* h1_ready = nullptr,
+                        const Drafts* drafts = nullptr) {
   const ls_config& c = s->cfg;
   const LayerOff& o = s->off[l];
   const int d = c.d_model, F = c.d_ff, mt = c.mma_dtype, pt = c.dtype;
@@ -449,7 +475,7 @@ ls_status block_forward(const ls_stage* s, int l, int T, const FwdBufs& f, const
   // kernel.  Serving: in the epilogue only where it is fused there; otherwise the kernel that writes K and V
   // to the pages rotates q and k in the same pass (where the projection has too few tiles for the fused epilogue, a
   // rotary kernel of its own before the page write cost 13 us per block of d 4096 and 512 rows).
-  const bool roped = !gpt && mt != LS_F32 && (!kv || gemm_qkv_rope_fuses(mt, T, d, c.head_dim, true));
+  const bool roped = !gpt && mt != LS_F32 && !drafts && (!kv || gemm_qkv_rope_fuses(mt, T, d, c.head_dim, true));
   // Serving calls whose projection is split over k: one kernel sums the parts, rotates q and k and writes the pages (in
   // place of a reduce kernel and the rotary / page kernel).  LS_ESTATE from the split-K launcher means "this shape is
   // not split": the plain path runs instead.  Any other status is a failure of the launch itself and ends the call.
@@ -468,7 +494,7 @@ ls_status block_forward(const ls_stage* s, int l, int T, const FwdBufs& f, const
   if (roped) {
     LS_TRY(lsk_gemm_qkv_rope(mt, T, d, f.h1, wptr(s, o.w_qkv), f.qkv, c.n_heads, c.head_dim, pos, s->rope_table, st));
   } else {
-    if ((((uintptr_t)kp | (uintptr_t)vp) & 7) == 0)   // four values a store
+    if (!drafts && (((uintptr_t)kp | (uintptr_t)vp) & 7) == 0)   // four values a store; drafted rows go to slots of their own
       LS_TRY(split(3 * d, d, f.h1, wptr(s, o.w_qkv), &split_qkv));
     if (!split_qkv) {
       LS_TRY(linear(s, T, 3 * d, d, f.h1, wptr(s, o.w_qkv), f.qkv, mt, gpt ? pptr(s, o.b_qkv) : nullptr, nullptr,
@@ -476,7 +502,9 @@ ls_status block_forward(const ls_stage* s, int l, int T, const FwdBufs& f, const
       if (!gpt && !kv) LS_TRY(lsk_rope(f.qkv, mt, T, c.n_heads, c.head_dim, pos, s->rope_table, 1.0f, st));
     }
   }
-  if (kv) {
+  if (drafts) {
+    LS_TRY(verify_attention(s, T, f, pos, req, B, kv, kp, vp, *drafts, st));
+  } else if (kv) {
     if (split_qkv)
       LS_TRY(lsk_finish_qkv(f.scratch, splits, T, c.n_heads, c.head_dim, gpt ? pptr(s, o.b_qkv) : nullptr, pt, pos, req,
                             gpt ? nullptr : s->rope_table, f.qkv, mt, kp, vp, kv->block_table, kv->max_pages_per_req,
@@ -536,7 +564,7 @@ bool fused_decode_ok(const ls_stage* s, int T) {
 
 ls_status block_forward_fused(const ls_stage* s, int l, int T, const FwdBufs& f, const int32_t* pos, const int32_t* req,
                               int B, const ls_kv* kv, int max_ctx, const int32_t* chunk_start, int n_decode,
-                              hipStream_t st) {
+                              hipStream_t st, const Drafts* drafts = nullptr) {
   const ls_config& c = s->cfg;
   const LayerOff& o = s->off[l];
   const int d = c.d_model, F = c.d_ff, mt = c.mma_dtype, pt = c.dtype;
@@ -550,11 +578,16 @@ ls_status block_forward_fused(const ls_stage* s, int l, int T, const FwdBufs& f,
   const size_t slab = (size_t)kv->n_pages * c.n_heads * c.page_size * c.head_dim * osz(s);
   void* kp = (char*)kv->k_pool + (size_t)l * slab;
   void* vp = (char*)kv->v_pool + (size_t)l * slab;
-  LS_TRY(lsk_gemm_partials(mt, T, 3 * d, d, f.h1, d, wptr(s, o.w_qkv), d, f.scratch, sf, &splits, st));
-  LS_TRY(lsk_finish_qkv(f.scratch, splits, T, c.n_heads, c.head_dim, gpt ? pptr(s, o.b_qkv) : nullptr, pt, pos, req,
-                        gpt ? nullptr : s->rope_table, f.qkv, mt, kp, vp, kv->block_table, kv->max_pages_per_req,
-                        c.page_size, st));
-  LS_TRY(serve_attention(s, T, f, pos, req, B, kv, kp, vp, max_ctx, chunk_start, n_decode, st));
+  if (drafts) {   // the kernel that sums the projection's parts writes rows to their positions, not to slots of their own
+    LS_TRY(linear(s, T, 3 * d, d, f.h1, wptr(s, o.w_qkv), f.qkv, mt, gpt ? pptr(s, o.b_qkv) : nullptr, nullptr, f.scratch, st));
+    LS_TRY(verify_attention(s, T, f, pos, req, B, kv, kp, vp, *drafts, st));
+  } else {
+    LS_TRY(lsk_gemm_partials(mt, T, 3 * d, d, f.h1, d, wptr(s, o.w_qkv), d, f.scratch, sf, &splits, st));
+    LS_TRY(lsk_finish_qkv(f.scratch, splits, T, c.n_heads, c.head_dim, gpt ? pptr(s, o.b_qkv) : nullptr, pt, pos, req,
+                          gpt ? nullptr : s->rope_table, f.qkv, mt, kp, vp, kv->block_table, kv->max_pages_per_req,
+                          c.page_size, st));
+    LS_TRY(serve_attention(s, T, f, pos, req, B, kv, kp, vp, max_ctx, chunk_start, n_decode, st));
+  }
   LS_TRY(lsk_gemm_partials(mt, T, d, d, f.o, d, wptr(s, o.w_o), d, f.scratch, sf, &splits, st));
   LS_TRY(lsk_finish_resid_norm(f.scratch, splits, T, d, gpt ? pptr(s, o.b_o) : nullptr, f.x, f.x1, nk, pptr(s, o.n2_g),
                                gpt ? pptr(s, o.n2_b) : nullptr, pt, c.norm_eps, f.h2, mt, st));
@@ -626,13 +659,14 @@ ls_status check_kv(const ls_stage* s, const ls_kv* kv, int B, const int32_t* new
 }
 
 ls_status serve_forward(ls_stage* s, const void* X, int T, int B, const ls_kv* kv, int max_ctx, void* Y,
-                        const FwdWs& w, const int32_t* chunk_start, int n_decode, hipStream_t st) {
+                        const FwdWs& w, const int32_t* chunk_start, int n_decode, hipStream_t st,
+                        const Drafts* drafts = nullptr) {
   const ls_config& c = s->cfg;
   LS_TRY(lsk_convert(X, c.io_dtype, w.xa, LS_F32, (size_t)T * c.d_model, st));
-  const bool gemv = decode_gemv_covers(c.mma_dtype, c.dtype, T, c.d_model, c.d_ff, c.head_dim);
+  const bool gemv = !drafts && decode_gemv_covers(c.mma_dtype, c.dtype, T, c.d_model, c.d_ff, c.head_dim);
   // pools that are not 8-byte aligned go where they went without these kernels: a page write that takes any alignment, or
   // one that refuses them
-  const bool rows = !gemv && (((uintptr_t)kv->k_pool | (uintptr_t)kv->v_pool) & 7) == 0 &&
+  const bool rows = !drafts && !gemv && (((uintptr_t)kv->k_pool | (uintptr_t)kv->v_pool) & 7) == 0 &&
                     decode_rows_covers(c.mma_dtype, c.dtype, T, c.d_model, c.d_ff, c.head_dim);
   const bool fused = fused_decode_ok(s, T);
   bool h1_ready = false;
@@ -640,8 +674,8 @@ ls_status serve_forward(ls_stage* s, const void* X, int T, int B, const ls_kv* k
     FwdBufs f{w.xa, w.xb, w.xa, nullptr, nullptr, nullptr, nullptr, nullptr,
               w.h, w.qkv, w.o, w.h, w.up, w.act, w.scratch};
     if (gemv || rows) LS_TRY(block_forward_few(s, l, T, f, w.pos, w.req, B, kv, max_ctx, chunk_start, n_decode, rows, st));
-    else if (fused) LS_TRY(block_forward_fused(s, l, T, f, w.pos, w.req, B, kv, max_ctx, chunk_start, n_decode, st));
-    else LS_TRY(block_forward(s, l, T, f, w.pos, w.req, B, 0, kv, max_ctx, chunk_start, n_decode, st, &h1_ready));
+    else if (fused) LS_TRY(block_forward_fused(s, l, T, f, w.pos, w.req, B, kv, max_ctx, chunk_start, n_decode, st, drafts));
+    else LS_TRY(block_forward(s, l, T, f, w.pos, w.req, B, 0, kv, max_ctx, chunk_start, n_decode, st, &h1_ready, drafts));
   }
   return lsk_convert(w.xa, LS_F32, Y, c.io_dtype, (size_t)T * c.d_model, st);
 }
@@ -830,6 +864,35 @@ ls_status stage_step(ls_stage* s, const void* X, int n_decode, const int32_t* ch
   LS_CHECK_LAUNCH();
   // without prompt chunks this is a decode step (no chunk table: every row goes to the decode kernel)
   return serve_forward(s, X, T, B, kv, max_ctx, Y, w, n_prefill > 0 ? ch.start : nullptr, n_decode, st);
+}
+
+ls_status stage_verify(ls_stage* s, const void* X, const int32_t* parent, const int32_t* start, const int32_t* n_nodes, int B,
+                       const ls_kv* kv, void* Y, void* workspace, void* stream) {
+  LS_TRY(check_stage(s, true));
+  LS_REQUIRE(X && parent && start && n_nodes && Y && workspace, "stage_verify: null argument");
+  LS_REQUIRE(B > 0 && B <= 65535, "stage_verify: B must be in 1..65535, got %d", B);
+  int max_nodes = 0, max_ctx = 0;
+  long rows = 0;
+  for (int b = 0; b < B; ++b) {
+    LS_REQUIRE(n_nodes[b] > 0 && n_nodes[b] <= kMaxNodes, "stage_verify: request %d has %d nodes, not 1..%d", b, n_nodes[b],
+               kMaxNodes);
+    if (n_nodes[b] > max_nodes) max_nodes = n_nodes[b];
+    rows += n_nodes[b];
+  }
+  LS_TRY(check_kv(s, kv, B, n_nodes, &max_ctx));
+  const int T = (int)rows;
+  hipStream_t st = (hipStream_t)stream;
+  FwdWs w;
+  carve_fwd(s, workspace, T, &w);
+  LS_TRY(lsk_tree_index(parent, start, kv->ctx_len, B, T, max_nodes, w.pos, w.slot, w.req, w.mask, stream));
+  int max_past = max_ctx;   // without lengths on the host: what a row of the block table holds
+  if (kv->ctx_len_host) {
+    max_past = 0;
+    for (int b = 0; b < B; ++b)
+      if (kv->ctx_len_host[b] > max_past) max_past = kv->ctx_len_host[b];
+  }
+  const Drafts drafts = {start, w.slot, w.mask, max_nodes, max_past};
+  return serve_forward(s, X, T, B, kv, max_ctx, Y, w, nullptr, 0, st, &drafts);
 }
 
 ls_status stage_train_fwd(ls_stage* s, const void* X, int B, int L, void* Y, void* saved, void* workspace,

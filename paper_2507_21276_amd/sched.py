@@ -217,3 +217,54 @@ class Server:
 
     def in_flight(self):
         return Bd.lib().ls_server_in_flight(self.h)
+
+
+class Pages:
+    """Books over the pages of a pool (ls_pages_* of include/lemix_serve.h).  grow and compact return the (sources,
+    destinations) of the page copies that lsk_kv_copy_pages has to make."""
+
+    def __init__(self, n_pages, page_size, max_rows, max_pages_per_row):
+        self.n_pages, self.max_rows, self.max_pages = n_pages, max_rows, max_pages_per_row
+        self.h = C.c_void_p()
+        self._destroy = Bd.lib().ls_pages_destroy
+        Bd._check(Bd.lib().ls_pages_create(n_pages, page_size, max_rows, max_pages_per_row, C.byref(self.h)))
+
+    def close(self):
+        if getattr(self, "h", None):
+            self._destroy(self.h)
+            self.h = None
+
+    __del__ = close
+
+    def available(self):
+        return Bd.lib().ls_pages_available(self.h)
+
+    def row(self, row):
+        ids, n = (C.c_int32 * self.max_pages)(), C.c_int()
+        Bd._check(Bd.lib().ls_pages_row(self.h, row, ids, C.byref(n)))
+        return list(ids[:n.value])
+
+    def table(self):
+        """Page ids [max_rows][max_pages_per_row], 0 past a row's last page: the block table to send to the device."""
+        ids, out = (C.c_int32 * self.max_pages)(), []
+        for r in range(self.max_rows):
+            Bd._check(Bd.lib().ls_pages_row(self.h, r, ids, None))
+            out.append(list(ids))
+        return out
+
+    def _pairs(self, capacity, call):
+        src, dst, n = (C.c_int32 * capacity)(), (C.c_int32 * capacity)(), C.c_int()
+        Bd._check(call(src, dst, C.byref(n)))
+        return list(src[:n.value]), list(dst[:n.value])
+
+    def grow(self, row, written_from, n_tokens):
+        return self._pairs(self.max_pages, lambda *a: Bd.lib().ls_pages_grow(self.h, row, written_from, n_tokens, *a))
+
+    def fork(self, from_row, to_row, n_tokens):
+        Bd._check(Bd.lib().ls_pages_fork(self.h, from_row, to_row, n_tokens))
+
+    def truncate(self, row, n_tokens):
+        Bd._check(Bd.lib().ls_pages_truncate(self.h, row, n_tokens))
+
+    def compact(self):
+        return self._pairs(self.n_pages, lambda *a: Bd.lib().ls_pages_compact(self.h, *a))
