@@ -242,20 +242,30 @@ __global__ __launch_bounds__(256, 2) void tree_attn_kernel(const T* __restrict__
     for (int j = 0; j < DT; ++j) oacc[n][j] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
 
-  // A tile's rows lie in groups of eight on one page each: their offsets in the pools, and which of them lie on no page
+  // A tile's rows lie in groups of eight on one page each: the pages' ids, read a tile before they are needed, then the groups'
+  // offsets in the pools and which of them lie on no page
+  struct Ids { int v[4]; };
   struct Where { long at[4]; int bad; };
   const int last_page = (nkeys - 1) >> shift;
-  auto find = [&](int t, Where& w) {
+  auto look_up = [&](int t) {
+    Ids ids;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) ids.v[i] = bt[min((t * 32 + i * 8) >> shift, last_page)];
+    return ids;
+  };
+  auto find = [&](int t, const Ids& ids) {
+    Where w;
     w.bad = 0;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const int key = t * 32 + i * 8;
-      int id = bt[min(key >> shift, last_page)];
+      int id = ids.v[i];
       if ((unsigned)id >= (unsigned)tr.n_pages) { id = 0; w.bad |= 1 << i; }
-      w.at[i] = ((((long)id * hk + kvh) << shift) + (key & (page - 1))) * DH;
+      w.at[i] = ((((long)id * hk + kvh) << shift) + ((t * 32 + i * 8) & (page - 1))) * DH;
     }
+    return w;
   };
-  V8 kf[RW == 1 ? 2 * KS : NL], vf[NL];
+  // loads of a tile in registers: K as the lane's operand of the first product (RW = 1) or in whole rows, V in whole rows
+  struct Set { V8 k[RW == 1 ? 2 * KS : NL], v[NL]; int bad; };
   // row and piece of load j of this wavefront in whole-row order, and where its row group lies
   auto row_of = [&](int j) { return (rw * NL + j) * (64 / LPR) + lane / LPR; };
   auto group_at = [&](const Where& w, int j) {
@@ -263,36 +273,38 @@ __global__ __launch_bounds__(256, 2) void tree_attn_kernel(const T* __restrict__
     const int i = row_of(j) >> 3;
     return i < 2 ? (i == 0 ? a0 : a1) : (i == 2 ? a2 : a3);
   };
-  auto fetch_k = [&](const Where& w) {
+  auto fetch_k = [&](const Where& w, Set& set) {
     if constexpr (RW == 1) {   // the lane's operand of the first product
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
         const long a0 = w.at[2 * c], a1 = w.at[2 * c + 1];
         const T* kr = k_pool + ((lane >> 3) & 1 ? a1 : a0) + (lane & 7) * DH + quad * 8;
 #pragma unroll
-        for (int s = 0; s < KS; ++s) kf[c * KS + s] = *(const V8*)(kr + s * 32);
+        for (int s = 0; s < KS; ++s) set.k[c * KS + s] = *(const V8*)(kr + s * 32);
       }
     } else {
 #pragma unroll
       for (int j = 0; j < NL; ++j)
-        kf[j] = *(const V8*)(k_pool + group_at(w, j) + (row_of(j) & 7) * DH + (lane % LPR) * 8);
+        set.k[j] = *(const V8*)(k_pool + group_at(w, j) + (row_of(j) & 7) * DH + (lane % LPR) * 8);
     }
   };
-  auto fetch_v = [&](const Where& w) {
+  auto fetch_v = [&](const Where& w, Set& set) {
+    set.bad = w.bad;
 #pragma unroll
     for (int j = 0; j < NL; ++j)
-      vf[j] = *(const V8*)(v_pool + group_at(w, j) + (row_of(j) & 7) * DH + (lane % LPR) * 8);
+      set.v[j] = *(const V8*)(v_pool + group_at(w, j) + (row_of(j) & 7) * DH + (lane % LPR) * 8);
   };
   auto is_plain = [&](int t, int bad) { return t * 32 + 32 <= ctx && t * 32 + 32 <= k_hi && bad == 0; };   // all rows see all keys
   // V to LDS.  In the tiles that some row does not see whole, values that are not finite are left out of the product (0 * x
   // would reach the rows that do not see them); returns whether there were any.
-  auto put_v = [&](char* vt, int t, int bad) {
+  auto put_v = [&](char* vt, int t, const Set& set) {
     bool odd = false;
+    const int bad = set.bad;
     const bool plain = is_plain(t, bad);
 #pragma unroll
     for (int j = 0; j < NL; ++j) {
       const int r = row_of(j);
-      u32x4 v = __builtin_bit_cast(u32x4, vf[j]);
+      u32x4 v = __builtin_bit_cast(u32x4, set.v[j]);
       if (!plain) {
         const bool live = t * 32 + r < k_hi && !(bad >> (r >> 3) & 1);
         constexpr uint32_t E = Mma16<T>::kExp;
@@ -309,7 +321,7 @@ __global__ __launch_bounds__(256, 2) void tree_attn_kernel(const T* __restrict__
   };
 
   f32x4 sacc[NT][2];
-  auto first_product = [&](const char* kt) {
+  auto first_product = [&](const char* kt, const Set& set) {
 #pragma unroll
     for (int n = 0; n < NT; ++n) sacc[n][0] = sacc[n][1] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -317,7 +329,7 @@ __global__ __launch_bounds__(256, 2) void tree_attn_kernel(const T* __restrict__
 #pragma unroll
       for (int s = 0; s < KS; ++s) {
         V8 ka;
-        if constexpr (RW == 1) ka = kf[c * KS + s];
+        if constexpr (RW == 1) ka = set.k[c * KS + s];
         else ka = *(const V8*)(kt + k_at<DH>(16 * c + col, 4 * s + quad));
 #pragma unroll
         for (int n = 0; n < NT; ++n) sacc[n][c] = Mma16<T>::run(ka, qf[n][s], sacc[n][c]);
@@ -395,8 +407,7 @@ __global__ __launch_bounds__(256, 2) void tree_attn_kernel(const T* __restrict__
     }
     if (!plain && odd) {
       // Rare: values of this tile are infinite or NaN.  Key by key, what was left out is read again and added where it is seen.
-      Where w;
-      find(t, w);
+      const Where w = find(t, look_up(t));
 #pragma unroll 1
       for (int r = 0; r < 32; ++r) {
         if (k0 + r >= k_hi || (bad >> (r >> 3) & 1)) continue;
@@ -430,53 +441,63 @@ __global__ __launch_bounds__(256, 2) void tree_attn_kernel(const T* __restrict__
     char* vt = smem + wave * TILE;
     int t = t_lo + wave;
     if (t < t_hi) {
-      Where next;
-      find(t, next);
-      fetch_v(next);
-      fetch_k(next);
+      Set set;
+      Where next = find(t, look_up(t));
+      fetch_v(next, set);
+      fetch_k(next, set);
+      Ids ids = look_up(t + 4);
       for (; t < t_hi; t += 4) {
-        const int bad = next.bad;
+        const int bad = set.bad;
         const bool more = t + 4 < t_hi;
-        if (more) find(t + 4, next);
-        const bool odd = put_v(vt, t, bad);
-        if (more) fetch_v(next);
-        first_product(nullptr);
-        if (more) fetch_k(next);
+        next = find(t + 4, ids);
+        ids = look_up(t + 8);
+        const bool odd = put_v(vt, t, set);
+        if (more) fetch_v(next, set);
+        first_product(nullptr, set);
+        if (more) fetch_k(next, set);
         attend(vt, t, bad, odd);
       }
     }
   } else {
     if (threadIdx.x < 2 * KW) s_odd[threadIdx.x / KW][threadIdx.x % KW] = -1;
     __syncthreads();
-    Where next;
+    // two tiles in flight: the loads of a set are asked for again as soon as it is in LDS
+    Set set0, set1;
     int t = t_lo + kw;
-    if (t < t_hi) {
-      find(t, next);
-      fetch_v(next);
-      fetch_k(next);
-    }
-    for (int i = t_lo; i < t_hi; i += KW, t += KW) {   // the same number of trips in every wavefront
-      const int buf = (i - t_lo) / KW & 1, bad = next.bad;
+    Ids ids = look_up(t);
+    auto fetch = [&](int u, Set& set) {   // tile u, whose pages `ids` holds
+      if (u < t_hi) {
+        const Where w = find(u, ids);
+        fetch_v(w, set);
+        fetch_k(w, set);
+      }
+      ids = look_up(u + KW);
+    };
+    fetch(t, set0);
+    fetch(t + KW, set1);
+    auto step = [&](int buf, Set& set) {
       char* kt = smem + (buf * KW + kw) * 2 * TILE;
       char* vt = kt + TILE;
+      const int bad = set.bad;
       if (t < t_hi) {
-        if (put_v(vt, t, bad)) s_odd[buf][kw] = t;
+        if (put_v(vt, t, set)) s_odd[buf][kw] = t;
 #pragma unroll
-        for (int j = 0; j < NL; ++j) *(V8*)(kt + k_at<DH>(row_of(j), lane % LPR)) = kf[j];
+        for (int j = 0; j < NL; ++j) *(V8*)(kt + k_at<DH>(row_of(j), lane % LPR)) = set.k[j];
       }
-      if (t + KW < t_hi) {
-        find(t + KW, next);
-        fetch_v(next);
-        fetch_k(next);
-      }
+      fetch(t + 2 * KW, set);
       // all are past the tile before this one: its buffer is the next to be written
       __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
       __builtin_amdgcn_s_barrier();
       __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
-      if (t < t_hi) {
-        first_product(kt);
+      if (t < t_hi && row0 < rows) {
+        first_product(kt, set);
         attend(vt, t, bad, s_odd[buf][kw] == t);
       }
+      t += KW;
+    };
+    for (int i = t_lo; i < t_hi; i += 2 * KW) {   // the same number of trips in every wavefront
+      step(0, set0);
+      if (i + KW < t_hi) step(1, set1);
     }
   }
   // Join the KW sets, 16 rows of each wavefront at a time, through LDS
