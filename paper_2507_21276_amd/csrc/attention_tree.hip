@@ -180,14 +180,23 @@ template <int DH> __device__ __forceinline__ int k_at(int r, int c) {
   return r * (DH * 2) + ((c ^ x) << 4);
 }
 
+// Over the four quads of lanes that hold a row's scores: lane permutations without LDS
+__device__ __forceinline__ float quads_max(float v) {
+  auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+  a = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+}
+
 struct Parts {
   int n, keys;       // parts of a context, keys of each (the last takes the rest)
   int row_blocks;
   float* partial;    // [T][h][n][dh + 4]: output, maximum (base 2), sum
 };
 
+constexpr int tree_halves(int rw) { return rw == 4 ? 2 : 1; }   // of a tile, 32 keys each
 template <int DH, int RW> constexpr int tree_lds() {
-  constexpr int KW = 4 / RW, tile = 32 * DH * 2, work = RW == 1 ? 4 * tile : 2 * KW * 2 * tile, join = 4 * 16 * (DH + 4) * 4;
+  constexpr int KW = 4 / RW, tile = tree_halves(RW) * 32 * DH * 2, work = RW == 1 ? 4 * tile : 2 * KW * 2 * tile, join = 4 * 16 * (DH + 4) * 4;
   return work > join ? work : join;
 }
 
@@ -198,13 +207,14 @@ __global__ __launch_bounds__(256, 2) void tree_attn_kernel(const T* __restrict__
                                                            const uint64_t* __restrict__ masks, Tree tr, int h, int hk,
                                                            int shift, float scale_log2, Parts parts) {
   typedef typename Mma16<T>::V8 V8;
-  constexpr int KW = 4 / RW, ROWS = 16 * NT * RW;
+  constexpr int KW = 4 / RW, ROWS = 16 * NT * RW, H = tree_halves(RW), KEYS = 32 * H;
   constexpr int KS = DH / 32, DT = DH / 16, LPR = DH / 8;   // steps of the first product, of the second; lanes per row loaded
-  constexpr int NL = DH / 16 / RW;                          // loads of K, and of V, per wavefront and tile
-  constexpr int TILE = 32 * DH * 2;
+  constexpr int NL = H * DH / 16 / RW;                      // loads of K, and of V, per wavefront and tile
+  constexpr int G = 4 * H / RW;                             // groups of eight rows that a wavefront loads
+  constexpr int TILE = KEYS * DH * 2;
   __shared__ __attribute__((aligned(16))) char smem[tree_lds<DH, RW>()];
   __shared__ float s_m[4][NT * 16], s_l[4][NT * 16];
-  __shared__ int s_odd[2][KW];
+  __shared__ int s_flag[2][KW][RW];   // of the tile in a buffer: groups of rows on no page, and values that are not finite
 
   // Blocks of rows that read the same keys follow each other on one XCD (workgroups go round the eight of them)
   const int slot8 = blockIdx.x >> 3, item = (slot8 / parts.row_blocks) * 8 + (blockIdx.x & 7), rb = slot8 % parts.row_blocks;
@@ -217,7 +227,7 @@ __global__ __launch_bounds__(256, 2) void tree_attn_kernel(const T* __restrict__
   const int used = min(parts.n, max(1, (nkeys + parts.keys - 1) / parts.keys));   // parts of this request
   if (part >= used) return;
   const int k_lo = part * parts.keys, k_hi = part == used - 1 ? nkeys : k_lo + parts.keys;
-  const int t_lo = k_lo / 32, t_hi = (k_hi + 31) / 32;
+  const int t_lo = k_lo / KEYS, t_hi = (k_hi + KEYS - 1) / KEYS;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, col = lane & 15, quad = lane >> 4;
   const int rw = wave % RW, kw = wave / RW, row0 = rb * ROWS + rw * 16 * NT;
   const int32_t* bt = table + (long)b * tr.max_pages;
@@ -242,71 +252,79 @@ __global__ __launch_bounds__(256, 2) void tree_attn_kernel(const T* __restrict__
     for (int j = 0; j < DT; ++j) oacc[n][j] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
 
-  // A tile's rows lie in groups of eight on one page each: the pages' ids, read a tile before they are needed, then the groups'
-  // offsets in the pools and which of them lie on no page
-  struct Ids { int v[4]; };
-  struct Where { long at[4]; int bad; };
+  // A tile's rows lie in groups of eight on one page each: the ids of the pages of the wavefront's groups, read a tile before
+  // they are needed, then the groups' offsets in the pools and which of them lie on no page (bits of the tile's groups)
+  struct Ids { int v[G]; };
+  struct Where { long at[G]; int bad; };
   const int last_page = (nkeys - 1) >> shift;
   auto look_up = [&](int t) {
     Ids ids;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) ids.v[i] = bt[min((t * 32 + i * 8) >> shift, last_page)];
+    for (int i = 0; i < G; ++i) ids.v[i] = bt[min((t * KEYS + (rw * G + i) * 8) >> shift, last_page)];
     return ids;
   };
   auto find = [&](int t, const Ids& ids) {
     Where w;
     w.bad = 0;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < G; ++i) {
       int id = ids.v[i];
-      if ((unsigned)id >= (unsigned)tr.n_pages) { id = 0; w.bad |= 1 << i; }
-      w.at[i] = ((((long)id * hk + kvh) << shift) + ((t * 32 + i * 8) & (page - 1))) * DH;
+      if ((unsigned)id >= (unsigned)tr.n_pages) { id = 0; w.bad |= 1 << (rw * G + i); }
+      w.at[i] = ((((long)id * hk + kvh) << shift) + ((t * KEYS + (rw * G + i) * 8) & (page - 1))) * DH;
     }
     return w;
   };
   // loads of a tile in registers: K as the lane's operand of the first product (RW = 1) or in whole rows, V in whole rows
   struct Set { V8 k[RW == 1 ? 2 * KS : NL], v[NL]; int bad; };
-  // row and piece of load j of this wavefront in whole-row order, and where its row group lies
+  // Loads of whole rows: 64 lanes read 512 elements, 512 / DH rows, from one group of eight rows (head_dim 32: from two).  The
+  // group's offset is the wavefront's, the lane's place in it 8 lane elements.
   auto row_of = [&](int j) { return (rw * NL + j) * (64 / LPR) + lane / LPR; };
-  auto group_at = [&](const Where& w, int j) {
-    const long a0 = w.at[0], a1 = w.at[1], a2 = w.at[2], a3 = w.at[3];
-    const int i = row_of(j) >> 3;
-    return i < 2 ? (i == 0 ? a0 : a1) : (i == 2 ? a2 : a3);
+  auto rows_at = [&](const T* pool, const Where& w, int j) {
+    const int r = j * (64 / LPR);
+    if constexpr (DH == 32) {
+      const long lo = w.at[r >> 3], hi = w.at[(r >> 3) + 1];
+      return pool + (lane < 32 ? lo : hi) + (lane & 31) * 8;
+    } else {
+      return pool + w.at[r >> 3] + (r & 7) * DH + lane * 8;
+    }
+  };
+  // K and V that one workgroup reads are read past the caches
+  auto load = [&](const T* p) {
+    if constexpr (RW < 4) return __builtin_nontemporal_load((const V8*)p);
+    else return *(const V8*)p;
   };
   auto fetch_k = [&](const Where& w, Set& set) {
-    if constexpr (RW == 1) {   // the lane's operand of the first product
+    if constexpr (RW == 1) {
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
         const long a0 = w.at[2 * c], a1 = w.at[2 * c + 1];
         const T* kr = k_pool + ((lane >> 3) & 1 ? a1 : a0) + (lane & 7) * DH + quad * 8;
 #pragma unroll
-        for (int s = 0; s < KS; ++s) set.k[c * KS + s] = *(const V8*)(kr + s * 32);
+        for (int s = 0; s < KS; ++s) set.k[c * KS + s] = load(kr + s * 32);
       }
     } else {
 #pragma unroll
-      for (int j = 0; j < NL; ++j)
-        set.k[j] = *(const V8*)(k_pool + group_at(w, j) + (row_of(j) & 7) * DH + (lane % LPR) * 8);
+      for (int j = 0; j < NL; ++j) set.k[j] = load(rows_at(k_pool, w, j));
     }
   };
   auto fetch_v = [&](const Where& w, Set& set) {
     set.bad = w.bad;
 #pragma unroll
-    for (int j = 0; j < NL; ++j)
-      set.v[j] = *(const V8*)(v_pool + group_at(w, j) + (row_of(j) & 7) * DH + (lane % LPR) * 8);
+    for (int j = 0; j < NL; ++j) set.v[j] = load(rows_at(v_pool, w, j));
   };
-  auto is_plain = [&](int t, int bad) { return t * 32 + 32 <= ctx && t * 32 + 32 <= k_hi && bad == 0; };   // all rows see all keys
+  auto is_plain = [&](int t, int bad) { return (t + 1) * KEYS <= ctx && (t + 1) * KEYS <= k_hi && bad == 0; };   // all rows see all keys
   // V to LDS.  In the tiles that some row does not see whole, values that are not finite are left out of the product (0 * x
   // would reach the rows that do not see them); returns whether there were any.
-  auto put_v = [&](char* vt, int t, const Set& set) {
+  auto put_v = [&](auto plain_, char* vt, int t, const Set& set) {
     bool odd = false;
     const int bad = set.bad;
-    const bool plain = is_plain(t, bad);
+    const bool plain = decltype(plain_)::value || is_plain(t, bad);
 #pragma unroll
     for (int j = 0; j < NL; ++j) {
       const int r = row_of(j);
       u32x4 v = __builtin_bit_cast(u32x4, set.v[j]);
       if (!plain) {
-        const bool live = t * 32 + r < k_hi && !(bad >> (r >> 3) & 1);
+        const bool live = t * KEYS + r < k_hi && !(bad >> (r >> 3) & 1);
         constexpr uint32_t E = Mma16<T>::kExp;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
@@ -320,12 +338,12 @@ __global__ __launch_bounds__(256, 2) void tree_attn_kernel(const T* __restrict__
     return __builtin_amdgcn_ballot_w64(odd) != 0;
   };
 
-  f32x4 sacc[NT][2];
+  f32x4 sacc[NT][2 * H];
   auto first_product = [&](const char* kt, const Set& set) {
 #pragma unroll
-    for (int n = 0; n < NT; ++n) sacc[n][0] = sacc[n][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int c = 0; c < 2 * H; ++c) {
 #pragma unroll
-    for (int c = 0; c < 2; ++c)
+      for (int n = 0; n < NT; ++n) sacc[n][c] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int s = 0; s < KS; ++s) {
         V8 ka;
@@ -334,43 +352,47 @@ __global__ __launch_bounds__(256, 2) void tree_attn_kernel(const T* __restrict__
 #pragma unroll
         for (int n = 0; n < NT; ++n) sacc[n][c] = Mma16<T>::run(ka, qf[n][s], sacc[n][c]);
       }
+    }
   };
   // softmax and second product of tile t from the scores in sacc
-  auto attend = [&](const char* vt, int t, int bad, bool odd) {
-    const int k0 = t * 32;
-    const bool plain = is_plain(t, bad);
-    uint32_t seen[NT];   // bit r: the lane's row sees key k0 + r
+  auto attend = [&](auto plain_, const char* vt, int t, int bad, bool odd) {
+    const int k0 = t * KEYS;
+    const bool plain = decltype(plain_)::value || is_plain(t, bad);
+    uint64_t seen[NT];   // bit r: the lane's row sees key k0 + r
     if (!plain) {
-      uint32_t live = k_hi - k0 >= 32 ? ~0u : (1u << (k_hi - k0)) - 1;
+      uint64_t live = k_hi - k0 >= 64 ? ~0ull : (1ull << (k_hi - k0)) - 1;
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (bad >> i & 1) live &= ~(0xffu << (8 * i));
+      for (int i = 0; i < 4 * H; ++i)
+        if (bad >> i & 1) live &= ~(0xffull << (8 * i));
       const int nd0 = k0 - ctx, w0 = nd0 >> 6, sh = nd0 & 63;   // node of the tile's first key; negative: cached tokens come first
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
         const uint64_t* mask = masks + (size_t)(first + node[n]) * tr.words;
         uint64_t win = 0;
-        if (nd0 <= -32) win = ~0ull;
+        if (nd0 <= -64) win = ~0ull;
         else if (nd0 < 0) win = mask[0] << -nd0 | ((1ull << -nd0) - 1);
         else if (w0 < tr.words) {
           win = mask[w0] >> sh;
-          if (sh > 32 && w0 + 1 < tr.words) win |= mask[w0 + 1] << (64 - sh);
+          if (sh > 0 && w0 + 1 < tr.words) win |= mask[w0 + 1] << (64 - sh);
         }
-        seen[n] = (uint32_t)win & live;
+        seen[n] = win & live;
+        const uint64_t mine = seen[n] >> (4 * quad);
 #pragma unroll
-        for (int c = 0; c < 2; ++c)
+        for (int c = 0; c < 2 * H; ++c)
 #pragma unroll
           for (int i = 0; i < 4; ++i)
-            if (!(seen[n] >> (16 * c + 4 * quad + i) & 1)) sacc[n][c][i] = -INFINITY;
+            if (!(mine >> (16 * c + i) & 1)) sacc[n][c][i] = -INFINITY;
       }
     }
-    V8 pf[NT];
+    V8 pf[NT][H];
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
-      float mx = fmaxf(fmaxf(fmaxf(sacc[n][0][0], sacc[n][0][1]), fmaxf(sacc[n][0][2], sacc[n][0][3])),
-                       fmaxf(fmaxf(sacc[n][1][0], sacc[n][1][1]), fmaxf(sacc[n][1][2], sacc[n][1][3])));
-      mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
-      mx = fmaxf(mx, __shfl_xor(mx, 32, 64)) * scale_log2;
+      float mx = sacc[n][0][0];
+#pragma unroll
+      for (int c = 0; c < 2 * H; ++c)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) mx = fmaxf(mx, sacc[n][c][i]);
+      mx = quads_max(mx) * scale_log2;
       // The reference of the exponentials follows the maximum only when some row exceeds it by more than 2^8: until then the
       // weights stay at or below 256, inside every format, and nothing has to be rescaled.
       if (__builtin_amdgcn_ballot_w64(mx > m_run[n] + 8.f) != 0) {
@@ -385,39 +407,44 @@ __global__ __launch_bounds__(256, 2) void tree_attn_kernel(const T* __restrict__
       // weights below 2^-20 of the largest are lost.  The sums carry the same factor, which the division takes out.
       const float ref = (m_run[n] == -INFINITY ? 0.f : m_run[n]) - Mma16<T>::kLift;
 #pragma unroll
-      for (int c = 0; c < 2; ++c)
+      for (int c = 0; c < 2 * H; ++c)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(sacc[n][c][i], scale_log2, -ref));
           l_run[n] += p;
           sacc[n][c][i] = p;
-          pf[n][4 * c + i] = from_f<T>(p);   // the second product's operand: 16 bits, relative error of half a step each
+          pf[n][c >> 1][4 * (c & 1) + i] = from_f<T>(p);   // the second product's operand: 16 bits, relative error of half a step each
         }
     }
 #pragma unroll
-    for (int j = 0; j < DT; ++j) {
-      // keys 4 quad + (col / 4), head dimensions 16 j + 4 (col % 4) ..: the lane receives its column of the 4 x 16 block
-      const char* p0 = vt + v_at<DH>(4 * quad + (col >> 2), 2 * j + ((col >> 1) & 1)) + (col & 1) * 8;
-      const char* p1 = vt + v_at<DH>(16 + 4 * quad + (col >> 2), 2 * j + ((col >> 1) & 1)) + (col & 1) * 8;
-      const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)p0);
-      const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)p1);
-      const V8 vfrag = __builtin_bit_cast(V8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+    for (int hf = 0; hf < H; ++hf)
 #pragma unroll
-      for (int n = 0; n < NT; ++n) oacc[n][j] = Mma16<T>::run(vfrag, pf[n], oacc[n][j]);
-    }
+      for (int j = 0; j < DT; ++j) {
+        // keys 4 quad + (col / 4), head dimensions 16 j + 4 (col % 4) ..: the lane receives its column of the 4 x 16 block
+        const int r = 32 * hf + 4 * quad + (col >> 2), c = 2 * j + ((col >> 1) & 1);
+        const char* p0 = vt + v_at<DH>(r, c) + (col & 1) * 8;
+        const char* p1 = vt + v_at<DH>(r + 16, c) + (col & 1) * 8;
+        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)p0);
+        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)p1);
+        const V8 vfrag = __builtin_bit_cast(V8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+#pragma unroll
+        for (int n = 0; n < NT; ++n) oacc[n][j] = Mma16<T>::run(vfrag, pf[n][hf], oacc[n][j]);
+      }
     if (!plain && odd) {
       // Rare: values of this tile are infinite or NaN.  Key by key, what was left out is read again and added where it is seen.
-      const Where w = find(t, look_up(t));
 #pragma unroll 1
-      for (int r = 0; r < 32; ++r) {
-        if (k0 + r >= k_hi || (bad >> (r >> 3) & 1)) continue;
-        const long a0 = w.at[0], a1 = w.at[1], a2 = w.at[2], a3 = w.at[3];
-        const T* vr = v_pool + (r < 16 ? (r < 8 ? a0 : a1) : (r < 24 ? a2 : a3)) + (r & 7) * DH;
-        float p[NT];   // the weight of key r in the lane's row: held by the lane of that row and the key's quad
+      for (int r = 0; r < KEYS; ++r) {
+        const int key = k0 + r;
+        if (key >= k_hi || (bad >> (r >> 3) & 1)) continue;
+        const T* vr = v_pool + ((((long)bt[key >> shift] * hk + kvh) << shift) + (key & (page - 1))) * DH;
+        float p[NT];   // the weight of the key in the lane's row: held by the lane of that row and the key's quad
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
-          const f32x4 half = r < 16 ? sacc[n][0] : sacc[n][1];
-          const float x = (r & 2) ? ((r & 1) ? half[3] : half[2]) : ((r & 1) ? half[1] : half[0]);
+          f32x4 four = sacc[n][0];
+#pragma unroll
+          for (int c = 1; c < 2 * H; ++c)
+            if (r >> 4 == c) four = sacc[n][c];
+          const float x = (r & 2) ? ((r & 1) ? four[3] : four[2]) : ((r & 1) ? four[1] : four[0]);
           p[n] = __shfl(x, ((r >> 2) & 3) * 16 + col, 64);
         }
 #pragma unroll
@@ -435,9 +462,12 @@ __global__ __launch_bounds__(256, 2) void tree_attn_kernel(const T* __restrict__
     }
   };
 
+  const std::true_type plain_tile;
+  const std::false_type any_tile;
   if constexpr (RW == 1) {
     // The next tile's V is asked for as soon as this one's is in LDS, its K after the first product: a wavefront nearly
-    // always has a tile in flight
+    // always has a tile in flight.  The tiles that every row sees whole come first; from the first other one on (behind the
+    // context, or on a page that is not there) a second loop takes them all, so that its registers are not the first one's.
     char* vt = smem + wave * TILE;
     int t = t_lo + wave;
     if (t < t_hi) {
@@ -446,26 +476,27 @@ __global__ __launch_bounds__(256, 2) void tree_attn_kernel(const T* __restrict__
       fetch_v(next, set);
       fetch_k(next, set);
       Ids ids = look_up(t + 4);
-      for (; t < t_hi; t += 4) {
+      auto step = [&](auto plain_) {
         const int bad = set.bad;
         const bool more = t + 4 < t_hi;
         next = find(t + 4, ids);
         ids = look_up(t + 8);
-        const bool odd = put_v(vt, t, set);
+        const bool odd = put_v(plain_, vt, t, set);
         if (more) fetch_v(next, set);
         first_product(nullptr, set);
         if (more) fetch_k(next, set);
-        attend(vt, t, bad, odd);
-      }
+        attend(plain_, vt, t, bad, odd);
+        t += 4;
+      };
+      while (t < t_hi && is_plain(t, set.bad)) step(plain_tile);
+      while (t < t_hi) step(any_tile);
     }
   } else {
-    if (threadIdx.x < 2 * KW) s_odd[threadIdx.x / KW][threadIdx.x % KW] = -1;
-    __syncthreads();
-    // two tiles in flight: the loads of a set are asked for again as soon as it is in LDS
-    Set set0, set1;
+    // The loads of a set are asked for again as soon as it is in LDS; head_dim 128 has registers for one set of 64 keys
+    Set set;
     int t = t_lo + kw;
     Ids ids = look_up(t);
-    auto fetch = [&](int u, Set& set) {   // tile u, whose pages `ids` holds
+    auto fetch = [&](int u) {   // tile u, whose pages `ids` holds
       if (u < t_hi) {
         const Where w = find(u, ids);
         fetch_v(w, set);
@@ -473,31 +504,29 @@ __global__ __launch_bounds__(256, 2) void tree_attn_kernel(const T* __restrict__
       }
       ids = look_up(u + KW);
     };
-    fetch(t, set0);
-    fetch(t + KW, set1);
-    auto step = [&](int buf, Set& set) {
+    fetch(t);
+    for (int i = t_lo, buf = 0; i < t_hi; i += KW, buf ^= 1, t += KW) {   // the same number of trips in every wavefront
       char* kt = smem + (buf * KW + kw) * 2 * TILE;
       char* vt = kt + TILE;
-      const int bad = set.bad;
       if (t < t_hi) {
-        if (put_v(vt, t, set)) s_odd[buf][kw] = t;
+        const bool odd = put_v(any_tile, vt, t, set);
 #pragma unroll
         for (int j = 0; j < NL; ++j) *(V8*)(kt + k_at<DH>(row_of(j), lane % LPR)) = set.k[j];
+        if (lane == 0) s_flag[buf][kw][rw] = set.bad | (int)odd << 8;
       }
-      fetch(t + 2 * KW, set);
+      fetch(t + KW);
       // all are past the tile before this one: its buffer is the next to be written
       __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
       __builtin_amdgcn_s_barrier();
       __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
       if (t < t_hi && row0 < rows) {
+        int flags = 0;
+#pragma unroll
+        for (int w = 0; w < RW; ++w) flags |= s_flag[buf][kw][w];
+        flags = __builtin_amdgcn_readfirstlane(flags);
         first_product(kt, set);
-        attend(vt, t, bad, s_odd[buf][kw] == t);
+        attend(any_tile, vt, t, flags & 255, flags >> 8);
       }
-      t += KW;
-    };
-    for (int i = t_lo; i < t_hi; i += 2 * KW) {   // the same number of trips in every wavefront
-      step(0, set0);
-      if (i + KW < t_hi) step(1, set1);
     }
   }
   // Join the KW sets, 16 rows of each wavefront at a time, through LDS
@@ -591,7 +620,7 @@ Plan plan(int B, int hk, int g, int dh, int max_nodes, int max_ctx) {
   const int rows = max_nodes * g, tiles = rows <= 16 ? 1 : 2, row_waves = rows <= 32 ? 1 : rows <= 64 || dh == 32 ? 2 : 4;
   Plan p = {tiles, row_waves, (rows + 16 * tiles * row_waves - 1) / (16 * tiles * row_waves), 1};
   const long groups = (long)B * hk * p.row_blocks, keys = (long)max_ctx + max_nodes;
-  long n = (2048 + groups - 1) / groups;
+  long n = groups >= 1024 ? 1 : (2048 + groups - 1) / groups;
   if (n > (keys + 255) / 256) n = (keys + 255) / 256;
   p.parts = (int)(n > 1 ? n : 1);
   return p;
