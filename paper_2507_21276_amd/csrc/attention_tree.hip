@@ -242,6 +242,11 @@ __global__ __launch_bounds__(256, 2) void tree_attn_kernel(const T* __restrict__
 #pragma unroll
     for (int s = 0; s < KS; ++s) qf[n][s] = *(const V8*)(qr + s * 32 + quad * 8);
   }
+  // Q has arrived before any tile is asked for: its first use in the loop would otherwise wait for the newest loads as well
+#pragma unroll
+  for (int n = 0; n < NT; ++n)
+#pragma unroll
+    for (int s = 0; s < KS; ++s) asm volatile("" : "+v"(qf[n][s]));
   f32x4 oacc[NT][DT];
   float m_run[NT], l_run[NT];
 #pragma unroll
@@ -312,52 +317,82 @@ __global__ __launch_bounds__(256, 2) void tree_attn_kernel(const T* __restrict__
 #pragma unroll
     for (int j = 0; j < NL; ++j) set.v[j] = load(rows_at(v_pool, w, j));
   };
+  // A lane's byte offsets in the tiles.  Both swizzles are an exclusive or of the piece with row bits that a load, a step of a
+  // product or a half of the tile does not touch, or only as a constant: the other offsets follow from these.
+  const int v_put = v_at<DH>(lane / LPR, lane % LPR) + rw * NL * 1024, k_put = k_at<DH>(lane / LPR, lane % LPR) + rw * NL * 1024;
+  const int v_get = v_at<DH>(4 * quad + (col >> 2), (col >> 1) & 1) + (col & 1) * 8, k_get = k_at<DH>(col, quad);
+  auto v_put_at = [&](int j) { return (v_put ^ (DH == 128 ? (j & 1) << 7 : 0)) + j * 1024; };
+  auto k_put_at = [&](int j) { return (k_put ^ (DH == 128 ? (j & 3) << 6 : DH == 64 ? (j & 1) << 6 : 0)) + j * 1024; };
   auto is_plain = [&](int t, int bad) { return (t + 1) * KEYS <= ctx && (t + 1) * KEYS <= k_hi && bad == 0; };   // all rows see all keys
   // V to LDS.  In the tiles that some row does not see whole, values that are not finite are left out of the product (0 * x
   // would reach the rows that do not see them); returns whether there were any.
   auto put_v = [&](auto plain_, char* vt, int t, const Set& set) {
-    bool odd = false;
     const int bad = set.bad;
-    const bool plain = decltype(plain_)::value || is_plain(t, bad);
+    if (decltype(plain_)::value || is_plain(t, bad)) {
+#pragma unroll
+      for (int j = 0; j < NL; ++j) *(V8*)(vt + v_put_at(j)) = set.v[j];
+      return false;
+    }
+    bool odd = false;
 #pragma unroll
     for (int j = 0; j < NL; ++j) {
       const int r = row_of(j);
       u32x4 v = __builtin_bit_cast(u32x4, set.v[j]);
-      if (!plain) {
-        const bool live = t * KEYS + r < k_hi && !(bad >> (r >> 3) & 1);
-        constexpr uint32_t E = Mma16<T>::kExp;
+      const bool live = t * KEYS + r < k_hi && !(bad >> (r >> 3) & 1);
+      constexpr uint32_t E = Mma16<T>::kExp;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const bool lo = (v[e] & E) == E, hi = (v[e] >> 16 & E) == E;
-          odd |= live && (lo || hi);
-          v[e] = !live ? 0u : v[e] & (lo ? 0xffff0000u : ~0u) & (hi ? 0x0000ffffu : ~0u);
-        }
+      for (int e = 0; e < 4; ++e) {
+        const bool lo = (v[e] & E) == E, hi = (v[e] >> 16 & E) == E;
+        odd |= live && (lo || hi);
+        v[e] = !live ? 0u : v[e] & (lo ? 0xffff0000u : ~0u) & (hi ? 0x0000ffffu : ~0u);
       }
-      *(u32x4*)(vt + v_at<DH>(r, lane % LPR)) = v;
+      *(u32x4*)(vt + v_put_at(j)) = v;
     }
     return __builtin_amdgcn_ballot_w64(odd) != 0;
   };
 
   f32x4 sacc[NT][2 * H];
   auto first_product = [&](const char* kt, const Set& set) {
+    V8 ka[2][KS];   // from LDS 16 keys ahead
+    int at = k_get;
+    asm volatile("" : "+v"(at));   // the few offsets are made anew: held over the loop they are registers that spill
+    auto read_k = [&](int c) {
+#pragma unroll
+      for (int s = 0; s < KS; ++s) ka[c & 1][s] = *(const V8*)(kt + (at ^ (s << 6)) + c * 16 * DH * 2);
+    };
+    if constexpr (RW > 1) read_k(0);
 #pragma unroll
     for (int c = 0; c < 2 * H; ++c) {
+      if constexpr (RW > 1) {
+        if (c + 1 < 2 * H) read_k(c + 1);
+        __builtin_amdgcn_sched_barrier(0);
+      }
 #pragma unroll
       for (int n = 0; n < NT; ++n) sacc[n][c] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int s = 0; s < KS; ++s) {
-        V8 ka;
-        if constexpr (RW == 1) ka = set.k[c * KS + s];
-        else ka = *(const V8*)(kt + k_at<DH>(16 * c + col, 4 * s + quad));
+      for (int s = 0; s < KS; ++s)
 #pragma unroll
-        for (int n = 0; n < NT; ++n) sacc[n][c] = Mma16<T>::run(ka, qf[n][s], sacc[n][c]);
-      }
+        for (int n = 0; n < NT; ++n) sacc[n][c] = Mma16<T>::run(RW == 1 ? set.k[c * KS + s] : ka[c & 1][s], qf[n][s], sacc[n][c]);
     }
   };
   // softmax and second product of tile t from the scores in sacc
   auto attend = [&](auto plain_, const char* vt, int t, int bad, bool odd) {
     const int k0 = t * KEYS;
     const bool plain = decltype(plain_)::value || is_plain(t, bad);
+    // Operand of the second product: keys 4 quad + (col / 4), head dimensions 16 j + 4 (col % 4) ..: the lane receives its column
+    // of the 4 x 16 block.  Those of the first 32 keys are read behind the softmax, the others as registers come free.
+    V8 vf[DT];
+    int at = v_get;
+    asm volatile("" : "+v"(at));
+    auto read_v = [&](int hf, int j) {
+      const char* p0 = vt + (at ^ (j << 5)) + hf * 32 * DH * 2;
+      const char* p1 = p0 + 16 * DH * 2;
+      const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)p0);
+      const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)p1);
+      vf[j] = __builtin_bit_cast(V8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+    };
+#pragma unroll
+    for (int j = 0; j < DT; ++j) read_v(0, j);
     uint64_t seen[NT];   // bit r: the lane's row sees key k0 + r
     if (!plain) {
       uint64_t live = k_hi - k0 >= 64 ? ~0ull : (1ull << (k_hi - k0)) - 1;
@@ -387,11 +422,11 @@ __global__ __launch_bounds__(256, 2) void tree_attn_kernel(const T* __restrict__
     V8 pf[NT][H];
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
-      float mx = sacc[n][0][0];
+      float mc[2 * H];
 #pragma unroll
-      for (int c = 0; c < 2 * H; ++c)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) mx = fmaxf(mx, sacc[n][c][i]);
+      for (int c = 0; c < 2 * H; ++c) mc[c] = fmaxf(fmaxf(sacc[n][c][0], sacc[n][c][1]), fmaxf(sacc[n][c][2], sacc[n][c][3]));
+      float mx = fmaxf(mc[0], mc[1]);
+      if constexpr (H == 2) mx = fmaxf(mx, fmaxf(mc[2], mc[3]));
       mx = quads_max(mx) * scale_log2;
       // The reference of the exponentials follows the maximum only when some row exceeds it by more than 2^8: until then the
       // weights stay at or below 256, inside every format, and nothing has to be rescaled.
@@ -411,24 +446,22 @@ __global__ __launch_bounds__(256, 2) void tree_attn_kernel(const T* __restrict__
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(sacc[n][c][i], scale_log2, -ref));
-          l_run[n] += p;
           sacc[n][c][i] = p;
           pf[n][c >> 1][4 * (c & 1) + i] = from_f<T>(p);   // the second product's operand: 16 bits, relative error of half a step each
         }
+      float lc[2 * H];
+#pragma unroll
+      for (int c = 0; c < 2 * H; ++c) lc[c] = (sacc[n][c][0] + sacc[n][c][1]) + (sacc[n][c][2] + sacc[n][c][3]);
+      if constexpr (H == 2) l_run[n] += (lc[0] + lc[1]) + (lc[2] + lc[3]);
+      else l_run[n] += lc[0] + lc[1];
     }
 #pragma unroll
     for (int hf = 0; hf < H; ++hf)
 #pragma unroll
       for (int j = 0; j < DT; ++j) {
-        // keys 4 quad + (col / 4), head dimensions 16 j + 4 (col % 4) ..: the lane receives its column of the 4 x 16 block
-        const int r = 32 * hf + 4 * quad + (col >> 2), c = 2 * j + ((col >> 1) & 1);
-        const char* p0 = vt + v_at<DH>(r, c) + (col & 1) * 8;
-        const char* p1 = vt + v_at<DH>(r + 16, c) + (col & 1) * 8;
-        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)p0);
-        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)p1);
-        const V8 vfrag = __builtin_bit_cast(V8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
 #pragma unroll
-        for (int n = 0; n < NT; ++n) oacc[n][j] = Mma16<T>::run(vfrag, pf[n][hf], oacc[n][j]);
+        for (int n = 0; n < NT; ++n) oacc[n][j] = Mma16<T>::run(vf[j], pf[n][hf], oacc[n][j]);
+        if (hf + 1 < H) read_v(hf + 1, j);
       }
     if (!plain && odd) {
       // Rare: values of this tile are infinite or NaN.  Key by key, what was left out is read again and added where it is seen.
@@ -440,11 +473,13 @@ __global__ __launch_bounds__(256, 2) void tree_attn_kernel(const T* __restrict__
         float p[NT];   // the weight of the key in the lane's row: held by the lane of that row and the key's quad
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
-          f32x4 four = sacc[n][0];
+          float x = 0.f;
 #pragma unroll
-          for (int c = 1; c < 2 * H; ++c)
-            if (r >> 4 == c) four = sacc[n][c];
-          const float x = (r & 2) ? ((r & 1) ? four[3] : four[2]) : ((r & 1) ? four[1] : four[0]);
+          for (int c = 0; c < 2 * H; ++c)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              if ((r >> 4) == c && (r & 3) == i) x = to_f(pf[n][c >> 1][4 * (c & 1) + i]);
+          x = fmaxf(x, 1e-30f);   // a weight that its 16 bits do not hold is still positive (NaN becomes 1e-30, its sum is NaN)
           p[n] = __shfl(x, ((r >> 2) & 3) * 16 + col, 64);
         }
 #pragma unroll
@@ -492,38 +527,46 @@ __global__ __launch_bounds__(256, 2) void tree_attn_kernel(const T* __restrict__
       while (t < t_hi) step(any_tile);
     }
   } else {
-    // The loads of a set are asked for again as soon as it is in LDS; head_dim 128 has registers for one set of 64 keys
+    // whether any page of this part is not there: the flags of plain tiles are not looked at otherwise
+    bool gaps = false;
+    for (int p = (k_lo >> shift) + threadIdx.x; p <= (k_hi - 1) >> shift; p += 256) gaps |= (unsigned)bt[p] >= (unsigned)tr.n_pages;
+    const bool any_gap = __syncthreads_or(gaps);
+    // The loads of a tile are asked for as soon as the one before it is in LDS
     Set set;
     int t = t_lo + kw;
     Ids ids = look_up(t);
-    auto fetch = [&](int u) {   // tile u, whose pages `ids` holds
-      if (u < t_hi) {
-        const Where w = find(u, ids);
-        fetch_v(w, set);
-        fetch_k(w, set);
-      }
-      ids = look_up(u + KW);
-    };
-    fetch(t);
+    if (t < t_hi) {
+      const Where w = find(t, ids);
+      fetch_v(w, set);
+      fetch_k(w, set);
+    }
+    ids = look_up(t + KW);
     for (int i = t_lo, buf = 0; i < t_hi; i += KW, buf ^= 1, t += KW) {   // the same number of trips in every wavefront
       char* kt = smem + (buf * KW + kw) * 2 * TILE;
       char* vt = kt + TILE;
+      const Where next = find(t + KW, ids);   // of ids that came during the tile before this one: no wait behind the stores
       if (t < t_hi) {
         const bool odd = put_v(any_tile, vt, t, set);
 #pragma unroll
-        for (int j = 0; j < NL; ++j) *(V8*)(kt + k_at<DH>(row_of(j), lane % LPR)) = set.k[j];
+        for (int j = 0; j < NL; ++j) *(V8*)(kt + k_put_at(j)) = set.k[j];
         if (lane == 0) s_flag[buf][kw][rw] = set.bad | (int)odd << 8;
       }
-      fetch(t + KW);
+      if (t + KW < t_hi) {
+        fetch_v(next, set);
+        fetch_k(next, set);
+      }
+      ids = look_up(t + 2 * KW);
       // all are past the tile before this one: its buffer is the next to be written
       __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
       __builtin_amdgcn_s_barrier();
       __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
       if (t < t_hi && row0 < rows) {
         int flags = 0;
+        if (any_gap || !is_plain(t, 0)) {
 #pragma unroll
-        for (int w = 0; w < RW; ++w) flags |= s_flag[buf][kw][w];
-        flags = __builtin_amdgcn_readfirstlane(flags);
+          for (int w = 0; w < RW; ++w) flags |= s_flag[buf][kw][w];
+          flags = __builtin_amdgcn_readfirstlane(flags);
+        }
         first_product(kt, set);
         attend(any_tile, vt, t, flags & 255, flags >> 8);
       }
