@@ -656,16 +656,25 @@ __global__ __launch_bounds__(256) void tree_merge_kernel(T* __restrict__ o, long
     if (DH >= 64 || lane < DH) o[(long)t * ldo + (long)head * DH + lane + 64 * i] = from_f<T>(l == 0.f ? 0.f : v[i] / l);
 }
 
-// Rows of a workgroup (tiles of 16 a wavefront, wavefronts with rows of their own), blocks of rows, parts of the contexts
+// Rows of a workgroup (tiles of 16 a wavefront, wavefronts with rows of their own), blocks of rows, parts of the contexts.
+// How far the other contexts fall short of the longest is not known here, so a rule has to hold for equal ones and for one
+// long one among short ones (up to a sixteenth).  us, equal | one long, 8 nodes, 32 heads of 128 unless said:
+//   A split costs a launch (one request of 256 tokens 1/8.5, 2/11.3; 1024 1/15, 8/10.4) and the partial results.  Workgroups
+//   fill the chip from about 512 on (4 requests of 4096: 1/68 | 60, 4/50 | 39, 16/55 | 24), with 128 keys or more each.
+//   Beyond that only so that one long context is not the last workgroup's for itself: parts of 2048 keys below 512 pairs (4
+//   requests of 16384 2/165 | 125, 8/173 | 74; five query heads a key head, 64 nodes, 16 requests 1/636 | 417, 4/542 | 134, 8/562
+//   | 114), of 4096 from there on (64 requests of 16384 1/2551 | 277, 4/2737 | 211, 8/2864 | 171; of 4096 1/649 | 74, 2/714 | 71).
 struct Plan { int tiles, row_waves, row_blocks, parts; };
 Plan plan(int B, int hk, int g, int dh, int max_nodes, int max_ctx) {
   // head_dim 32: a tile is two loads, for two wavefronts
   const int rows = max_nodes * g, tiles = rows <= 16 ? 1 : 2, row_waves = rows <= 32 ? 1 : rows <= 64 || dh == 32 ? 2 : 4;
   Plan p = {tiles, row_waves, (rows + 16 * tiles * row_waves - 1) / (16 * tiles * row_waves), 1};
-  const long groups = (long)B * hk * p.row_blocks, keys = (long)max_ctx + max_nodes;
-  long n = groups >= 1024 ? 1 : (2048 + groups - 1) / groups;
-  if (n > (keys + 255) / 256) n = (keys + 255) / 256;
-  p.parts = (int)(n > 1 ? n : 1);
+  const long pairs = (long)B * hk * p.row_blocks, keys = (long)max_ctx + max_nodes;
+  if (keys <= 512) return p;
+  const long fill = 512 / pairs, most = pairs < 512 ? 2048 : 4096, even = (keys + most / 2) / most;
+  long n = fill > even ? fill : even;
+  if (n > keys / 128) n = keys / 128;
+  if (n > 1) p.parts = n < 4096 ? (int)n : 4096;
   return p;
 }
 
