@@ -624,36 +624,55 @@ __global__ __launch_bounds__(256, 2) void tree_attn_kernel(const T* __restrict__
   }
 }
 
-// Joins the parts of a (row, head), in their order; a wavefront each
+// Joins the parts of a request's rows, in a fixed order: a wavefront has a (row, head), DH / 4 lanes have a part, four of its
+// values each.  `blocks` workgroups belong to a request, so that no wavefront has to search for its own; a lane holds the
+// maximum and sum of one part while the outputs are on their way (600 rows x 40 heads of up to eight parts: 22 -> 16 us).
 template <class T, int DH>
-__global__ __launch_bounds__(256) void tree_merge_kernel(T* __restrict__ o, long ldo, Tree tr, int h, int hk, int shift, Parts parts) {
-  const long item = (long)blockIdx.x * 4 + (threadIdx.x >> 6);
-  const int t = (int)(item / h), head = (int)(item % h), lane = threadIdx.x & 63;
-  if (t >= min(tr.start[tr.B], tr.T) || t < tr.start[0]) return;
-  const int b = request_of(tr.start, tr.B, t), first = tr.start[b];
-  const int nodes = min(min(tr.start[b + 1], tr.T) - first, tr.max_nodes);
-  if (t - first >= nodes) return;
+__global__ __launch_bounds__(256) void tree_merge_kernel(T* __restrict__ o, long ldo, Tree tr, int h, int shift, int blocks,
+                                                         Parts parts) {
+  constexpr int LP = DH / 4, AT = 64 / LP;
+  const int b = blockIdx.x / blocks, lane = threadIdx.x & 63;
+  const long item = (long)(blockIdx.x % blocks) * 4 + (threadIdx.x >> 6);   // of the request's nodes x heads
+  const int first = tr.start[b], nodes = min(min(tr.start[b + 1], tr.T) - first, tr.max_nodes);
+  if (first < 0 || item >= (long)nodes * h) return;
   const int nkeys = (int)min((long)max(tr.ctx_len[b], 0) + nodes, (long)tr.max_pages << shift);
   const int used = min(parts.n, max(1, (nkeys + parts.keys - 1) / parts.keys));
   if (used == 1) return;   // written already
-  const float* pp = parts.partial + item * parts.n * (DH + 4);
-  float m = -INFINITY, l = 0.f, v[(DH + 63) / 64];
-  for (int s = lane; s < used; s += 64) m = fmaxf(m, pp[s * (DH + 4) + DH]);
-  m = wave_max(m);
-  const float ref = m == -INFINITY ? 0.f : m;
+  const long t = first + item / h, head = item % h;
+  const float* pp = parts.partial + (t * h + head) * parts.n * (DH + 4);
+  float m = -INFINITY, l = 0.f;
+  f32x4 v = f32x4{0.f, 0.f, 0.f, 0.f};
+  for (int s0 = 0; s0 < used; s0 += 64) {
+    const int n = min(64, used - s0);
+    const float ms = lane < n ? pp[(long)(s0 + lane) * (DH + 4) + DH] : -INFINITY;
+    const float ls = lane < n ? pp[(long)(s0 + lane) * (DH + 4) + DH + 1] : 0.f;
+    const float m_new = fmaxf(m, wave_max(ms)), ref = m_new == -INFINITY ? 0.f : m_new, alpha = __builtin_amdgcn_exp2f(m - ref);
+    const float f = __builtin_amdgcn_exp2f(ms - ref);
+    m = m_new;
+    l = l * alpha + wave_sum(ls * f);
+    v *= alpha;
+    for (int s = 0; s < n; s += 4 * AT) {
+      f32x4 x[4];
 #pragma unroll
-  for (int i = 0; i < (DH + 63) / 64; ++i) v[i] = 0.f;
-#pragma unroll 4
-  for (int s = 0; s < used; ++s) {
-    const float f = __builtin_amdgcn_exp2f(pp[s * (DH + 4) + DH] - ref);
-    l += pp[s * (DH + 4) + DH + 1] * f;
+      for (int i = 0; i < 4; ++i) x[i] = *(const f32x4*)(pp + (long)(s0 + min(s + i * AT + lane / LP, n - 1)) * (DH + 4) + (lane % LP) * 4);
 #pragma unroll
-    for (int i = 0; i < (DH + 63) / 64; ++i)
-      if (DH >= 64 || lane < DH) v[i] += pp[s * (DH + 4) + lane + 64 * i] * f;
+      for (int i = 0; i < 4; ++i) {
+        const int at = s + i * AT + lane / LP;
+        const float fs = __shfl(f, at, 64);
+        if (at < n) v += x[i] * fs;
+      }
+    }
   }
 #pragma unroll
-  for (int i = 0; i < (DH + 63) / 64; ++i)
-    if (DH >= 64 || lane < DH) o[(long)t * ldo + (long)head * DH + lane + 64 * i] = from_f<T>(l == 0.f ? 0.f : v[i] / l);
+  for (int off = LP; off < 64; off <<= 1)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] += __shfl_xor(v[i], off, 64);
+  if (lane >= LP) return;
+  typedef T V4 __attribute__((ext_vector_type(4)));
+  V4 out;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) out[i] = from_f<T>(l == 0.f ? 0.f : v[i] / l);
+  *(V4*)(o + t * ldo + head * DH + lane * 4) = out;
 }
 
 // Rows of a workgroup (tiles of 16 a wavefront, wavefronts with rows of their own), blocks of rows, parts of the contexts.
@@ -731,14 +750,15 @@ ls_status lsk_attn_tree(const void* q, long ldq, int dt, int T, int B, int max_n
     LS_REQUIRE(groups <= 0x7fffffffL, "attn_tree: too many (request, head) pairs");
     const dim3 grid((unsigned)groups, p.parts);
     const int shift = __builtin_ctz(page);
+    const long merge = ((long)max_nodes * h + 3) / 4;   // workgroups a request
+    LS_REQUIRE(merge * B <= 0x7fffffffL, "attn_tree: too many (row, head) pairs");
     auto go = [&](auto* one_, auto dh_, auto nt_, auto rw_) {
       typedef std::remove_pointer_t<decltype(one_)> T_;
       constexpr int DH = decltype(dh_)::value, NT = decltype(nt_)::value, RW = decltype(rw_)::value;
       tree_attn_kernel<T_, DH, NT, RW><<<grid, 256, 0, st>>>((const T_*)q, ldq, (T_*)o, ldo, (const T_*)k_pool,
                                                            (const T_*)v_pool, block_table, mask, tr, h, hk, shift, scale_log2,
                                                            parts);
-      if (p.parts > 1)
-        tree_merge_kernel<T_, DH><<<(unsigned)(((long)T * h + 3) / 4), 256, 0, st>>>((T_*)o, ldo, tr, h, hk, shift, parts);
+      if (p.parts > 1) tree_merge_kernel<T_, DH><<<(unsigned)(B * merge), 256, 0, st>>>((T_*)o, ldo, tr, h, shift, (int)merge, parts);
     };
     auto rows = [&](auto* one_, auto dh_) {
       const std::integral_constant<int, 1> c1;

@@ -24,34 +24,53 @@ __global__ __launch_bounds__(256) void copy_pages_kernel(char* k_pool, char* v_p
 
 // Rows ctx + path[i] -> ctx + i of one request, all layers and heads.  A thread owns one 16-byte column of the row and walks
 // the path itself: nodes rise along it, so path[i] >= i, no row is read after it was overwritten, and no order between
-// threads matters.  One workgroup per (256 columns, K / V and layer, request).
+// threads matters.  Eight nodes at a time, whose path entries, page ids and rows are each asked for together: one node after
+// the other is three round trips each (paths of up to five nodes, 32 requests, two layers of 32 heads x 128: 8.2 -> 5.9 us).
+// One workgroup per (256 columns, K / V and layer, request).
 __global__ __launch_bounds__(256) void move_rows_kernel(char* k_pool, char* v_pool, const int32_t* block_table,
                                                         const int32_t* ctx_len, const int32_t* path, int max_path,
                                                         const int32_t* n_path, int h, int page, int row_bytes, int max_pages,
                                                         int n_pages, size_t slab_bytes) {
+  constexpr int N = 8;
   const int b = blockIdx.z, l = blockIdx.y >> 1, per = row_bytes / 16;
   const int col = blockIdx.x * 256 + threadIdx.x;
   if (col >= h * per) return;
   char* pool = ((blockIdx.y & 1) ? v_pool : k_pool) + (size_t)l * slab_bytes;
-  const int head = col / per, piece = col % per;
   const int32_t* row = block_table + (size_t)b * max_pages;
+  const int32_t* nodes = path + (size_t)b * max_path;
   const int ctx = ctx_len[b], n = min(n_path[b], max_path);
   if (ctx < 0) return;
-  auto at = [&](int slot) -> char* {
-    const int id = row[slot / page];
-    if ((unsigned)id >= (unsigned)n_pages) return nullptr;
-    return pool + (((size_t)id * h + head) * page + slot % page) * row_bytes + piece * 16;
-  };
+  // the slot's place in a head's column of its page; the page's id comes from the table
+  auto within = [&](int slot) { return ((size_t)(col / per) * page + slot % page) * row_bytes + (col % per) * 16; };
+  const size_t page_bytes = (size_t)h * page * row_bytes;
   const long room = (long)max_pages * page;
   int prev = -1;
-  for (int i = 0; i < n; ++i) {
-    const int node = path[(size_t)b * max_path + i];
-    if (node <= prev || (long)ctx + node >= room) return;   // not a path: what is left stays where it is
-    prev = node;
-    if (node == i) continue;
-    const char* src = at(ctx + node);
-    char* dst = at(ctx + i);
-    if (src && dst) *(u32x4*)dst = *(const u32x4*)src;
+  for (int i0 = 0; i0 < n; i0 += N) {
+    int node[N], from[N], to[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) node[i] = i0 + i < n ? nodes[i0 + i] : -1;
+    int live = 0;   // nodes of the eight that belong to the path: it ends at the first that does not rise or has no slot
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const bool ok = live == i && node[i] > prev && (long)ctx + node[i] < room;
+      live += ok;
+      if (ok) prev = node[i];
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const bool moves = i < live && node[i] != i0 + i;
+      from[i] = moves ? row[(ctx + node[i]) / page] : -1;
+      to[i] = moves ? row[(ctx + i0 + i) / page] : -1;
+    }
+    u32x4 v[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      if ((unsigned)from[i] < (unsigned)n_pages) v[i] = *(const u32x4*)(pool + from[i] * page_bytes + within(ctx + node[i]));
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      if ((unsigned)from[i] < (unsigned)n_pages && (unsigned)to[i] < (unsigned)n_pages)
+        *(u32x4*)(pool + to[i] * page_bytes + within(ctx + i0 + i)) = v[i];
+    if (live < N) return;
   }
 }
 
