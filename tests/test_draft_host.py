@@ -139,3 +139,32 @@ def test_scratch_sizes_of_empty_calls_are_zero():
     assert lib.lsk_qk_norm_rope_bwd_partial_floats(0, 4, 4, 64) == 0
     assert lib.lsk_qk_norm_rope_bwd_partial_floats(5, 4, 4, 64) > 0
     assert lib.lsk_attn_tree_scratch_floats(0, 0, 4, 4, 64, 8, 100) == 0
+
+
+def test_stage_verify_validates_its_arguments_before_any_launch():
+    """An fp32 stage without a rotary table allocates nothing on the device."""
+    from paper_2507_21276_amd import synth_inputs as S
+    lib = Bd.lib()
+    c, h = Bd.make_config(S.CONFIGS["tiny_gpt_f32"]), C.c_void_p()
+    assert lib.ls_create(C.byref(c), C.byref(h)) == Bd.LS_OK
+    ctx = (C.c_int32 * 2)(10, 30)
+    kv = Bd.ls_kv(P, P, P, P, C.cast(ctx, C.c_void_p), 8, 3)   # rows of three pages of 16
+
+    def call(n=(1, 2), X=P, parent=P, start=P, kv=kv, Y=P, ws=P, B=None):
+        return lib.stage_verify(h, X, parent, start, ints(n), len(n) if B is None else B, C.byref(kv), Y, ws, None)
+
+    assert lib.stage_verify(None, P, P, P, ints([1]), 1, C.byref(kv), P, P, None) == Bd.LS_EINVAL
+    assert call() == Bd.LS_ESTATE                      # no parameters bound yet
+    assert lib.ls_bind_params(h, P, None) == Bd.LS_OK
+    for over in (dict(X=None), dict(parent=None), dict(start=None), dict(Y=None), dict(ws=None)):
+        assert call(**over) == Bd.LS_EINVAL and "null" in err()
+    assert lib.stage_verify(h, P, P, P, None, 2, C.byref(kv), P, P, None) == Bd.LS_EINVAL and "null" in err()
+    for B in (0, -1, 65536):
+        assert call(B=B) == Bd.LS_EINVAL and "B must be" in err()
+    assert call(n=(0, 1)) == Bd.LS_EINVAL and "nodes" in err()
+    assert call(n=(1, 257)) == Bd.LS_EINVAL and "nodes" in err()
+    assert call(n=(1, 19)) == Bd.LS_EINVAL and "block table" in err()          # 30 + 19 tokens on three pages
+    ctx[0] = -1
+    assert call() == Bd.LS_EINVAL and "negative" in err()
+    assert call(kv=Bd.ls_kv(P, P, None, P, None, 8, 3)) == Bd.LS_EINVAL and "null field" in err()
+    lib.ls_destroy(h)

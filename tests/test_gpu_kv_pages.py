@@ -120,3 +120,42 @@ def test_a_captured_move_replays():
             ref = moved(ref, bt, past, paths, page)
             ref.view(torch.uint8)[:, spare[0]] = ref.view(torch.uint8)[:, int(bt[0, 1])].clone()
             assert torch.equal(bits(got), bits(ref))
+
+
+def test_pools_beyond_32_bits_of_elements():
+    """Pages at both ends of pools of more than 2^31 elements: written, attended to, copied and moved."""
+    h, page, dh, n_pages = 8, 16, 128, 140000
+    assert n_pages * h * page * dh > 2 ** 31
+    k = torch.empty(1, n_pages, h, page, dh, dtype=torch.float16, device="cuda")
+    v = torch.empty_like(k)
+    rng = np.random.default_rng(8)
+    bt = np.array([[n_pages - 1, 0, n_pages - 2], [1, n_pages - 3, 2]], np.int32)
+    past, counts, T = [30, 17], [3, 4], 7
+    qkv = torch.from_numpy(rng.standard_normal((T + 47, 3 * h * dh)).astype(np.float32)).half().cuda()
+    i32 = lambda a: torch.tensor(a, dtype=torch.int32, device="cuda")  # noqa: E731
+    q, table = torch.empty(T + 47, h * dh, dtype=torch.float16, device="cuda"), i32(bt)
+    # the contexts' rows, then the nodes'
+    req = [0] * 30 + [1] * 17 + [0] * 3 + [1] * 4
+    slot = list(range(30)) + list(range(17)) + [30, 31, 32] + [17, 18, 19, 20]
+    Bd.lsk_qk_norm_rope_kv_write(qkv, q, h, h, dh, None, i32(req), k[0], v[0], table, page, slot=i32(slot), norm=False)
+    keys, values = qkv[:, h * dh:2 * h * dh].reshape(-1, h, dh), qkv[:, 2 * h * dh:].reshape(-1, h, dh)
+    for t in (0, 29, 30, 46, 47, 53):
+        at = 0, int(bt[req[t], slot[t] // page]), slice(None), slot[t] % page
+        assert torch.equal(k[at], keys[t]) and torch.equal(v[at], values[t])
+    o = torch.empty(T, h * dh, dtype=torch.float16, device="cuda")
+    chains = [[0], [0, 1], [0, 1, 2], [0], [0, 1], [0, 1, 2], [0, 1, 2, 3]]
+    Bd.lsk_attn_tree(q[47:], o, h, h, dh, i32([0, 3, 7]), i32(past), torch.from_numpy(D.mask_words(chains, 1)).cuda(), 4, k[0], v[0],
+                     table, page, 30)
+    f64 = lambda x: x.cpu().double().numpy()  # noqa: E731
+    K, V, Q, O = f64(keys), f64(values), f64(q), f64(o)
+    for t in range(T):
+        b = 0 if t < 3 else 1
+        rows = [r for r in range(47) if req[r] == b] + [47 + (0 if b == 0 else 3) + j for j in chains[t]]
+        for head in (0, 7):
+            ref, tol = D.attend(Q[47 + t, head * dh:(head + 1) * dh], K[rows, head], V[rows, head], np.arange(len(rows)), "f16", D.HALF["f16"])
+            assert (np.abs(O[t, head * dh:(head + 1) * dh] - ref) <= tol).all()
+    kv, cfg = Bd.KV.of(k, v, table, past), config(1, h, dh, page, "f16")
+    Bd.lsk_kv_copy_pages(cfg, kv, [n_pages - 2, 1], [n_pages - 4, n_pages - 5])
+    assert torch.equal(bits(k[0, n_pages - 4]), bits(k[0, n_pages - 2])) and torch.equal(bits(v[0, n_pages - 5]), bits(v[0, 1]))
+    Bd.lsk_kv_move_rows(cfg, kv, i32([[2], [3]]), i32([1, 1]))      # slot 32 -> 30, slot 20 -> 17
+    assert torch.equal(k[0, 0, :, 14], keys[49]) and torch.equal(v[0, n_pages - 3, :, 1], values[53])
