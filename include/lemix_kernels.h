@@ -210,7 +210,8 @@ ls_status lsk_memory_available(size_t need_bytes, size_t threshold_bytes, int* a
  * lsk_kv_move_rows: accepts a path of each request's drafted tree: the rows of nodes path[b][i], i < n_path[b]
  * (path [dev] [B][max_path], n_path [dev] [B]), move from slot ctx_len[b] + path[b][i] to ctx_len[b] + i, so that the
  * context can be advanced by n_path[b].  Nodes rise along a path; a path is cut at the first node that does not, or whose
- * slot is beyond the block-table row.  Rows on pages whose id is outside 0..n_pages-1 are skipped.
+ * slot is beyond the block-table row.  Rows on pages whose id is outside 0..n_pages-1 are skipped.  The pages behind ctx_len[b]
+ * must be the request's own (ls_pages_grow sees to that).
  */
 ls_status lsk_kv_copy_pages(const ls_config* cfg, const ls_kv* kv, const int32_t* src, const int32_t* dst, int n,
                             void* stream);

@@ -76,7 +76,8 @@ __device__ __forceinline__ int request_of(const int32_t* start, int B, int t) {
   return lo;
 }
 
-// Any type and head size: a workgroup of four wavefronts per (row, head).  A wavefront takes 64 keys at a time, a lane one
+// Any type and head size: a workgroup of four wavefronts per (row, head), so that every row reads the keys for itself, through the
+// caches.  A wavefront takes 64 keys at a time, a lane one
 // key for the scores and a column (of up to four) for the outputs; the softmax is online per wavefront, the four are joined
 // through LDS.  Keys that the row does not see are left out of both products, whatever their rows hold.
 template <class T>
@@ -148,9 +149,13 @@ __global__ __launch_bounds__(256) void tree_attn_any_kernel(const T* q, long ldq
 // 16 + 4 q .. + 3 (q = lane / 16), and O^T += V^T P^T takes P from these very registers when V^T is fed in the same order of
 // keys, which two transposing LDS reads per 16 head dimensions do.
 //   RW = 1 (up to 32 rows): bound by the K and V bytes.  Each is loaded by one wavefront; K goes straight to registers as the
-//   first product's operand, V to the wavefront's own LDS buffer: no barrier in the loop.
+//   first product's operand, V to the wavefront's own LDS buffer: no barrier in the loop.  64 trees of 8 nodes, 32 heads of 128,
+//   16384 tokens each: 6.7 TB/s; of 128 to 2048 tokens 5.9 (216 us; with K and V read through the caches 239; two register sets
+//   of a tile and spills 330).
 //   RW = 2, 4 (more rows): bound by the exponentials and the products.  K and V tiles are loaded once for the RW wavefronts,
-//   through two LDS buffers and one barrier a tile.
+//   through two LDS buffers and one barrier a tile, of 64 keys where all four share it.  64 trees of 64 nodes, five query heads a
+//   key head, 16384 tokens each: 630 TFLOP/s; 12 of 40 - 61 nodes, 3000 to 16001 tokens: 480 (253 us; a wavefront with 64 rows of its
+//   own, which spills, 489; tiles of 32 keys 326).  The matrix cores are busy a third of the time, the vector units half.
 template <class T> struct Mma16;
 template <> struct Mma16<bf16_t> {
   typedef bf16x8 V8;

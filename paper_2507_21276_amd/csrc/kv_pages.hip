@@ -11,7 +11,9 @@ namespace {
 constexpr int kPairs = 256;   // page pairs passed by value to one launch
 struct Pairs { int32_t src[kPairs], dst[kPairs]; };
 
-// One workgroup per (pair, K / V and layer, piece of the page)
+// One workgroup per (pair, K / V and layer, piece of 16 KB of the page): 256 pages of 2 MB 214 us, 5.0 TB/s read and written
+// together, where a copy of 1 GB reaches 5.2.  Pairs come by value: no buffer to fill before the launch, and a captured call keeps
+// them.
 __global__ __launch_bounds__(256) void copy_pages_kernel(char* k_pool, char* v_pool, Pairs pr, size_t page_bytes,
                                                          size_t slab_bytes, int piece_bytes) {
   const int l = blockIdx.y >> 1;
