@@ -199,6 +199,77 @@ struct Parts {
   float* partial;    // [T][h][n][dh + 4]: output, maximum (base 2), sum
 };
 
+// A workgroup's rows: of request rows first .., `rows` (node, query head) pairs of key head kvh, from pair row0 on
+struct Rows { int first, rows, row0, kvh, g, h, used, part; };
+
+// Joins the 4 / RW sets of wavefronts, 16 rows of each wavefront at a time, through LDS, and stores the rows or the part's results.
+// oacc[n][j][i] is dimension 16 j + 4 quad + i of row 16 n + col, m_run and l_run its reference (base 2) and the lane's sum.
+template <class T, int DH, int NT, int RW>
+__device__ __forceinline__ void store_rows(const f32x4 (&oacc)[NT][DH / 16], const float (&m_run)[NT], const float (&l_run)[NT],
+                                           char* smem, float (&s_m)[4][NT * 16], float (&s_l)[4][NT * 16], const Rows& rw,
+                                           const Parts& parts, T* o, long ldo) {
+  constexpr int KW = 4 / RW, DT = DH / 16;
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, col = lane & 15, quad = lane >> 4;
+#pragma unroll
+  for (int n = 0; n < NT; ++n) {
+    float l = l_run[n] + __shfl_xor(l_run[n], 16, 64);
+    l += __shfl_xor(l, 32, 64);
+    if (quad == 0) { s_m[wave][n * 16 + col] = m_run[n]; s_l[wave][n * 16 + col] = l; }
+  }
+  float* so = (float*)smem;   // [wave][row][DH + 4]
+  constexpr int TPR = 16 / RW;   // threads a row
+  const int r = threadIdx.x / TPR, jw = r >> 4, jr = r & 15;
+#pragma unroll
+  for (int n = 0; n < NT; ++n) {
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < DT; ++j) *(f32x4*)(so + (wave * 16 + col) * (DH + 4) + 16 * j + 4 * quad) = oacc[n][j];
+    __syncthreads();
+    const int row = rw.row0 + (jw * NT + n) * 16 + jr;
+    if (row < rw.rows) {
+      float mm = -INFINITY, f[KW], l = 0.f;
+#pragma unroll
+      for (int w = 0; w < KW; ++w) mm = fmaxf(mm, s_m[w * RW + jw][n * 16 + jr]);
+      const float ref = mm == -INFINITY ? 0.f : mm;
+#pragma unroll
+      for (int w = 0; w < KW; ++w) {
+        f[w] = __builtin_amdgcn_exp2f(s_m[w * RW + jw][n * 16 + jr] - ref);   // a set without a tile: weight 0 and zeros
+        l += s_l[w * RW + jw][n * 16 + jr] * f[w];
+      }
+      const long trow = rw.first + row / rw.g, head = rw.kvh * rw.g + row % rw.g;
+      const float inv = 1.f / l;
+      float* pp = parts.partial + ((trow * rw.h + head) * parts.n + rw.part) * (DH + 4);
+      for (int c = (threadIdx.x % TPR) * 4; c < DH; c += 4 * TPR) {
+        f32x4 v = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int w = 0; w < KW; ++w) v += *(const f32x4*)(so + ((w * RW + jw) * 16 + jr) * (DH + 4) + c) * f[w];
+        if (rw.used == 1) {
+          typedef T V4 __attribute__((ext_vector_type(4)));
+          V4 out;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) out[i] = from_f<T>(l == 0.f ? 0.f : v[i] * inv);   // a row that sees nothing: zeros
+          *(V4*)(o + trow * ldo + head * DH + c) = out;
+        } else {
+          *(f32x4*)(pp + c) = v;
+        }
+      }
+      if (rw.used > 1 && threadIdx.x % TPR == 0) {
+        pp[DH] = mm;
+        pp[DH + 1] = l;
+      }
+    }
+  }
+}
+
+// Bits of 64 nodes from node nd0 on of a mask row: whether the row sees the key that lies there.  Below 0 lie cached tokens.
+__device__ __forceinline__ uint64_t window(const uint64_t* mask, int words, int nd0) {
+  const int w0 = nd0 >> 6, sh = nd0 & 63;
+  if (nd0 <= -64) return ~0ull;
+  if (nd0 < 0) return mask[0] << -nd0 | ((1ull << -nd0) - 1);
+  if (w0 >= words) return 0;
+  return mask[w0] >> sh | (sh > 0 && w0 + 1 < words ? mask[w0 + 1] << (64 - sh) : 0);
+}
+
 constexpr int tree_halves(int rw) { return rw == 4 ? 2 : 1; }   // of a tile, 32 keys each
 template <int DH, int RW> constexpr int tree_lds() {
   constexpr int KW = 4 / RW, tile = tree_halves(RW) * 32 * DH * 2, work = RW == 1 ? 4 * tile : 2 * KW * 2 * tile, join = 4 * 16 * (DH + 4) * 4;
@@ -404,17 +475,9 @@ __global__ __launch_bounds__(256, 2) void tree_attn_kernel(const T* __restrict__
 #pragma unroll
       for (int i = 0; i < 4 * H; ++i)
         if (bad >> i & 1) live &= ~(0xffull << (8 * i));
-      const int nd0 = k0 - ctx, w0 = nd0 >> 6, sh = nd0 & 63;   // node of the tile's first key; negative: cached tokens come first
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
-        const uint64_t* mask = masks + (size_t)(first + node[n]) * tr.words;
-        uint64_t win = 0;
-        if (nd0 <= -64) win = ~0ull;
-        else if (nd0 < 0) win = mask[0] << -nd0 | ((1ull << -nd0) - 1);
-        else if (w0 < tr.words) {
-          win = mask[w0] >> sh;
-          if (sh > 0 && w0 + 1 < tr.words) win |= mask[w0 + 1] << (64 - sh);
-        }
+        const uint64_t win = window(masks + (size_t)(first + node[n]) * tr.words, tr.words, k0 - ctx);
         seen[n] = win & live;
         const uint64_t mine = seen[n] >> (4 * quad);
 #pragma unroll
@@ -577,56 +640,193 @@ __global__ __launch_bounds__(256, 2) void tree_attn_kernel(const T* __restrict__
       }
     }
   }
-  // Join the KW sets, 16 rows of each wavefront at a time, through LDS
+  store_rows<T, DH, NT, RW>(oacc, m_run, l_run, smem, s_m, s_l, Rows{first, rows, rb * ROWS, kvh, g, h, used, part}, parts, o, ldo);
+}
+
+// ---- fp32 matrix-core kernel ---------------------------------------------------------------------
+//
+// The same split as RW = 1 with 16x16x4 fp32 products: 16 NT rows a workgroup, tiles of 16 keys shared out over the wavefronts.
+// A lane's K operand is a quarter of its key's row (the order of the contraction is free, so its four steps' worth are
+// contiguous), and the second product's steps take key 4 quad + i from the scores as they lie, V element by element from
+// memory, 64 bytes of a row for 16 lanes: nothing goes through LDS before the join.  Bound by the matrix instructions, which
+// take 32 cycles for 1024 multiply-adds, from two blocks of rows on, by loads before that: 16 trees of 16 nodes, 12 heads of 64,
+// 1024 tokens 26 us (4.0 TB/s), 300 with a workgroup a (row, head); 8 trees of 8, 4 heads of 32, 2048 tokens 14 and 214.
+template <int DH, int NT>
+__global__ __launch_bounds__(256, 2) void tree_attn_f32_kernel(const float* __restrict__ q, long ldq, float* __restrict__ o, long ldo,
+                                                               const float* __restrict__ k_pool, const float* __restrict__ v_pool,
+                                                               const int32_t* __restrict__ table, const uint64_t* __restrict__ masks,
+                                                               Tree tr, int h, int hk, int shift, float scale_log2, Parts parts) {
+  constexpr int ROWS = 16 * NT, DT = DH / 16, NK = DH / 16;   // 16-byte loads of a lane's quarter of a K row
+  __shared__ __attribute__((aligned(16))) char smem[4 * 16 * (DH + 4) * 4];
+  __shared__ float s_m[4][NT * 16], s_l[4][NT * 16];
+  const int slot8 = blockIdx.x >> 3, item = (slot8 / parts.row_blocks) * 8 + (blockIdx.x & 7), rb = slot8 % parts.row_blocks;
+  if (item >= tr.B * hk) return;
+  const int b = item / hk, kvh = item % hk, part = blockIdx.y, g = h / hk;
+  const int first = tr.start[b], nodes = min(min(tr.start[b + 1], tr.T) - first, tr.max_nodes), rows = nodes * g;
+  if (first < 0 || rb * ROWS >= rows) return;
+  const int ctx = max(tr.ctx_len[b], 0), page = 1 << shift;
+  const int nkeys = (int)min((long)ctx + nodes, (long)tr.max_pages * page);
+  const int used = min(parts.n, max(1, (nkeys + parts.keys - 1) / parts.keys));
+  if (part >= used) return;
+  const int k_lo = part * parts.keys, k_hi = part == used - 1 ? nkeys : k_lo + parts.keys;
+  const int t_lo = k_lo / 16, t_hi = (k_hi + 15) / 16;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, col = lane & 15, quad = lane >> 4;
+  const int32_t* bt = table + (long)b * tr.max_pages;
+
+  f32x4 qf[NT][NK];
+  int node[NT];
 #pragma unroll
   for (int n = 0; n < NT; ++n) {
-    float l = l_run[n] + __shfl_xor(l_run[n], 16, 64);
-    l += __shfl_xor(l, 32, 64);
-    if (quad == 0) { s_m[wave][n * 16 + col] = m_run[n]; s_l[wave][n * 16 + col] = l; }
+    const int r = min(rb * ROWS + n * 16 + col, rows - 1);
+    node[n] = r / g;
+    const float* qr = q + (long)(first + node[n]) * ldq + (long)(kvh * g + r % g) * DH + quad * (DH / 4);
+#pragma unroll
+    for (int s = 0; s < NK; ++s) qf[n][s] = *(const f32x4*)(qr + 4 * s);
   }
-  float* so = (float*)smem;   // [wave][row][DH + 4]
-  constexpr int TPR = 16 / RW;   // threads a row
-  const int r = threadIdx.x / TPR, jw = r >> 4, jr = r & 15;
+#pragma unroll
+  for (int n = 0; n < NT; ++n)
+#pragma unroll
+    for (int s = 0; s < NK; ++s) asm volatile("" : "+v"(qf[n][s]));   // Q is here before the first tile is asked for
+  f32x4 oacc[NT][DT];
+  float m_run[NT], l_run[NT];
 #pragma unroll
   for (int n = 0; n < NT; ++n) {
-    __syncthreads();
+    m_run[n] = -INFINITY;
+    l_run[n] = 0.f;
 #pragma unroll
-    for (int j = 0; j < DT; ++j) *(f32x4*)(so + (wave * 16 + col) * (DH + 4) + 16 * j + 4 * quad) = oacc[n][j];
-    __syncthreads();
-    const int row = rb * ROWS + (jw * NT + n) * 16 + jr;
-    if (row < rows) {
-      float mm = -INFINITY, f[KW], l = 0.f;
+    for (int j = 0; j < DT; ++j) oacc[n][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+
+  // the two groups of eight rows of a tile: their offsets in the pools, and which lie on no page
+  struct Where { long at[2]; int bad; };
+  const int last_page = (nkeys - 1) >> shift;
+  struct Ids { int v[2]; };
+  auto look_up = [&](int t) { return Ids{{bt[min((t * 16) >> shift, last_page)], bt[min((t * 16 + 8) >> shift, last_page)]}}; };
+  auto find = [&](int t, const Ids& ids) {
+    Where w;
+    w.bad = 0;
 #pragma unroll
-      for (int w = 0; w < KW; ++w) mm = fmaxf(mm, s_m[w * RW + jw][n * 16 + jr]);
-      const float ref = mm == -INFINITY ? 0.f : mm;
+    for (int i = 0; i < 2; ++i) {
+      int id = ids.v[i];
+      if ((unsigned)id >= (unsigned)tr.n_pages) { id = 0; w.bad |= 1 << i; }
+      w.at[i] = ((((long)id * hk + kvh) << shift) + ((t * 16 + i * 8) & (page - 1))) * DH;
+    }
+    return w;
+  };
+  f32x4 kf[NK];
+  float vf[DT][4];
+  int bad = 0;
+  auto fetch_k = [&](const Where& w) {
+    const long a0 = w.at[0], a1 = w.at[1];
+    const float* kr = k_pool + (col >= 8 ? a1 : a0) + (col & 7) * DH + quad * (DH / 4);
 #pragma unroll
-      for (int w = 0; w < KW; ++w) {
-        f[w] = __builtin_amdgcn_exp2f(s_m[w * RW + jw][n * 16 + jr] - ref);   // a set without a tile: weight 0 and zeros
-        l += s_l[w * RW + jw][n * 16 + jr] * f[w];
+    for (int s = 0; s < NK; ++s) kf[s] = *(const f32x4*)(kr + 4 * s);
+  };
+  auto fetch_v = [&](const Where& w) {
+    bad = w.bad;
+    const long a0 = w.at[0], a1 = w.at[1];
+    const float* vr = v_pool + (quad >= 2 ? a1 : a0) + (4 * quad & 7) * DH + col;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int j = 0; j < DT; ++j) vf[j][i] = vr[i * DH + 16 * j];
+  };
+
+  int t = t_lo + wave;
+  if (t < t_hi) {
+    Where next = find(t, look_up(t));
+    fetch_k(next);
+    fetch_v(next);
+    Ids ids = look_up(t + 4);
+    for (; t < t_hi; t += 4) {
+      const int k0 = t * 16;
+      const bool more = t + 4 < t_hi, plain = k0 + 16 <= ctx && k0 + 16 <= k_hi && bad == 0;   // plain: all rows see all keys
+      const int gaps = bad;
+      next = find(t + 4, ids);
+      ids = look_up(t + 8);
+      f32x4 p[NT];
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+        p[n] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int s = 0; s < NK; ++s)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) p[n] = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[s][e], qf[n][s][e], p[n], 0, 0, 0);
       }
-      const long trow = first + row / g, head = kvh * g + row % g;
-      const float inv = 1.f / l;
-      float* pp = parts.partial + ((trow * h + head) * parts.n + part) * (DH + 4);
-      for (int c = (threadIdx.x % TPR) * 4; c < DH; c += 4 * TPR) {
-        f32x4 v = f32x4{0.f, 0.f, 0.f, 0.f};
+      if (more) fetch_k(next);
+      uint32_t seen[NT];   // bit r: the lane's row sees key k0 + r
+      bool odd = false;
+      if (!plain) {
+        uint32_t live = k_hi - k0 >= 16 ? 0xffffu : (1u << (k_hi - k0)) - 1;
+        live &= (gaps & 1 ? 0xff00u : 0xffffu) & (gaps & 2 ? 0x00ffu : 0xffffu);
 #pragma unroll
-        for (int w = 0; w < KW; ++w) v += *(const f32x4*)(so + ((w * RW + jw) * 16 + jr) * (DH + 4) + c) * f[w];
-        if (used == 1) {
-          typedef T V4 __attribute__((ext_vector_type(4)));
-          V4 out;
+        for (int n = 0; n < NT; ++n) {
+          seen[n] = (uint32_t)window(masks + (size_t)(first + node[n]) * tr.words, tr.words, k0 - ctx) & live;
 #pragma unroll
-          for (int i = 0; i < 4; ++i) out[i] = from_f<T>(l == 0.f ? 0.f : v[i] * inv);   // a row that sees nothing: zeros
-          *(V4*)(o + trow * ldo + head * DH + c) = out;
-        } else {
-          *(f32x4*)(pp + c) = v;
+          for (int i = 0; i < 4; ++i)
+            if (!(seen[n] >> (4 * quad + i) & 1)) p[n][i] = -INFINITY;
         }
+        // values that are not finite are left out of the product, and added to the rows that see them afterwards
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int j = 0; j < DT; ++j) {
+            const bool here = live >> (4 * quad + i) & 1, finite = vf[j][i] - vf[j][i] == 0.f;
+            odd |= here && !finite;
+            if (!here || !finite) vf[j][i] = 0.f;
+          }
       }
-      if (used > 1 && threadIdx.x % TPR == 0) {
-        pp[DH] = mm;
-        pp[DH + 1] = l;
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+        const float mx = quads_max(fmaxf(fmaxf(p[n][0], p[n][1]), fmaxf(p[n][2], p[n][3]))) * scale_log2;
+        if (__builtin_amdgcn_ballot_w64(mx > m_run[n]) != 0) {
+          const float m_new = fmaxf(m_run[n], mx);
+          const float alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m_run[n] - m_new);
+          l_run[n] *= alpha;
+          m_run[n] = m_new;
+#pragma unroll
+          for (int j = 0; j < DT; ++j) oacc[n][j] *= alpha;
+        }
+        const float ref = m_run[n] == -INFINITY ? 0.f : m_run[n];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) p[n][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(p[n][i], scale_log2, -ref));
+        l_run[n] += (p[n][0] + p[n][1]) + (p[n][2] + p[n][3]);
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < DT; ++j)
+#pragma unroll
+          for (int n = 0; n < NT; ++n) oacc[n][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(vf[j][i], p[n][i], oacc[n][j], 0, 0, 0);
+      if (more) fetch_v(next);
+      if (!plain && __builtin_amdgcn_ballot_w64(odd) != 0) {
+#pragma unroll 1
+        for (int r = 0; r < 16; ++r) {
+          const int key = k0 + r;
+          if (key >= k_hi || (gaps >> (r >> 3) & 1)) continue;
+          const float* vr = v_pool + ((((long)bt[key >> shift] * hk + kvh) << shift) + (key & (page - 1))) * DH;
+          float w[NT];
+#pragma unroll
+          for (int n = 0; n < NT; ++n) {
+            const float x = (r & 2) ? ((r & 1) ? p[n][3] : p[n][2]) : ((r & 1) ? p[n][1] : p[n][0]);
+            w[n] = __shfl(fmaxf(x, 1e-30f), (r >> 2) * 16 + col, 64);
+          }
+#pragma unroll
+          for (int j = 0; j < DT; ++j)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const float v = vr[16 * j + 4 * quad + i];
+              if (v - v != 0.f) {
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+                  if (seen[n] >> r & 1) oacc[n][j][i] += w[n] * v;
+              }
+            }
+        }
       }
     }
   }
+  store_rows<float, DH, NT, 1>(oacc, m_run, l_run, smem, s_m, s_l, Rows{first, rows, rb * ROWS, kvh, g, h, used, part}, parts, o, ldo);
 }
 
 // Joins the parts of a request's rows, in a fixed order: a wavefront has a (row, head), DH / 4 lanes have a part, four of its
@@ -689,9 +889,10 @@ __global__ __launch_bounds__(256) void tree_merge_kernel(T* __restrict__ o, long
 //   requests of 16384 2/165 | 125, 8/173 | 74; five query heads a key head, 64 nodes, 16 requests 1/636 | 417, 4/542 | 134, 8/562
 //   | 114), of 4096 from there on (64 requests of 16384 1/2551 | 277, 4/2737 | 211, 8/2864 | 171; of 4096 1/649 | 74, 2/714 | 71).
 struct Plan { int tiles, row_waves, row_blocks, parts; };
-Plan plan(int B, int hk, int g, int dh, int max_nodes, int max_ctx) {
+Plan plan(int dt, int B, int hk, int g, int dh, int max_nodes, int max_ctx) {
   // head_dim 32: a tile is two loads, for two wavefronts
-  const int rows = max_nodes * g, tiles = rows <= 16 ? 1 : 2, row_waves = rows <= 32 ? 1 : rows <= 64 || dh == 32 ? 2 : 4;
+  const int rows = max_nodes * g, tiles = rows <= 16 ? 1 : 2;
+  const int row_waves = rows <= 32 || dt == LS_F32 ? 1 : rows <= 64 || dh == 32 ? 2 : 4;
   Plan p = {tiles, row_waves, (rows + 16 * tiles * row_waves - 1) / (16 * tiles * row_waves), 1};
   const long pairs = (long)B * hk * p.row_blocks, keys = (long)max_ctx + max_nodes;
   if (keys <= 512) return p;
@@ -722,8 +923,9 @@ ls_status lsk_tree_index(const int32_t* parent, const int32_t* start, const int3
 
 size_t lsk_attn_tree_scratch_floats(int T, int B, int h, int hk, int dh, int max_nodes, int max_ctx) {
   if (T <= 0 || B <= 0 || h <= 0 || hk <= 0 || h % hk || dh <= 0 || max_nodes <= 0 || max_ctx < 0) return 0;
-  const Plan p = plan(B, hk, h / hk, dh, max_nodes, max_ctx);
-  return p.parts > 1 ? (size_t)T * h * p.parts * (dh + 4) : 0;
+  const int a = plan(LS_F32, B, hk, h / hk, dh, max_nodes, max_ctx).parts, b = plan(LS_F16, B, hk, h / hk, dh, max_nodes, max_ctx).parts;
+  const int parts = a > b ? a : b;
+  return parts > 1 ? (size_t)T * h * parts * (dh + 4) : 0;
 }
 
 ls_status lsk_attn_tree(const void* q, long ldq, int dt, int T, int B, int max_nodes, int h, int hk, int dh,
@@ -742,9 +944,10 @@ ls_status lsk_attn_tree(const void* q, long ldq, int dt, int T, int B, int max_n
   const Tree tr = {start, ctx_len, mask, B, T, max_nodes, (max_nodes + 63) / 64, block_table, max_pages, page, n_pages};
   const float scale_log2 = 1.4426950408889634f / sqrtf((float)dh);
   hipStream_t st = (hipStream_t)stream;
-  if (dt != LS_F32 && (dh == 32 || dh == 64 || dh == 128) && page >= 8 && (page & (page - 1)) == 0 && ldq % 8 == 0 && ldo % 8 == 0 &&
+  const int per16 = dt == LS_F32 ? 4 : 8;   // elements of 16 bytes
+  if ((dh == 32 || dh == 64 || dh == 128) && page >= 8 && (page & (page - 1)) == 0 && ldq % per16 == 0 && ldo % per16 == 0 &&
       ((uintptr_t)q | (uintptr_t)o | (uintptr_t)k_pool | (uintptr_t)v_pool) % 16 == 0) {
-    Plan p = plan(B, hk, h / hk, dh, max_nodes, max_ctx);
+    Plan p = plan(dt, B, hk, h / hk, dh, max_nodes, max_ctx);
     const size_t one = (size_t)T * h * (dh + 4);
     const size_t room = scratch && (uintptr_t)scratch % 16 == 0 ? scratch_floats / one : 0;
     if ((size_t)p.parts > room) p.parts = room > 1 ? (int)room : 1;
@@ -760,26 +963,34 @@ ls_status lsk_attn_tree(const void* q, long ldq, int dt, int T, int B, int max_n
     auto go = [&](auto* one_, auto dh_, auto nt_, auto rw_) {
       typedef std::remove_pointer_t<decltype(one_)> T_;
       constexpr int DH = decltype(dh_)::value, NT = decltype(nt_)::value, RW = decltype(rw_)::value;
-      tree_attn_kernel<T_, DH, NT, RW><<<grid, 256, 0, st>>>((const T_*)q, ldq, (T_*)o, ldo, (const T_*)k_pool,
-                                                           (const T_*)v_pool, block_table, mask, tr, h, hk, shift, scale_log2,
-                                                           parts);
+      if constexpr (std::is_same_v<T_, float>)
+        tree_attn_f32_kernel<DH, NT><<<grid, 256, 0, st>>>((const float*)q, ldq, (float*)o, ldo, (const float*)k_pool,
+                                                         (const float*)v_pool, block_table, mask, tr, h, hk, shift, scale_log2, parts);
+      else
+        tree_attn_kernel<T_, DH, NT, RW><<<grid, 256, 0, st>>>((const T_*)q, ldq, (T_*)o, ldo, (const T_*)k_pool,
+                                                             (const T_*)v_pool, block_table, mask, tr, h, hk, shift, scale_log2,
+                                                             parts);
       if (p.parts > 1) tree_merge_kernel<T_, DH><<<(unsigned)(B * merge), 256, 0, st>>>((T_*)o, ldo, tr, h, shift, (int)merge, parts);
     };
     auto rows = [&](auto* one_, auto dh_) {
+      constexpr bool f32 = std::is_same_v<std::remove_pointer_t<decltype(one_)>, float>;
       const std::integral_constant<int, 1> c1;
       const std::integral_constant<int, 2> c2;
       const std::integral_constant<int, 4> c4;
       if (p.tiles == 1) go(one_, dh_, c1, c1);
       else if (p.row_waves == 1) go(one_, dh_, c2, c1);
-      else if (p.row_waves == 2) go(one_, dh_, c2, c2);
-      else if constexpr (decltype(dh_)::value > 32) go(one_, dh_, c2, c4);
+      else if constexpr (!f32) {
+        if (p.row_waves == 2) go(one_, dh_, c2, c2);
+        else if constexpr (decltype(dh_)::value > 32) go(one_, dh_, c2, c4);
+      }
     };
     auto size = [&](auto* one_) {
       if (dh == 32) rows(one_, std::integral_constant<int, 32>());
       else if (dh == 64) rows(one_, std::integral_constant<int, 64>());
       else rows(one_, std::integral_constant<int, 128>());
     };
-    if (dt == LS_BF16) size((bf16_t*)nullptr);
+    if (dt == LS_F32) size((float*)nullptr);
+    else if (dt == LS_BF16) size((bf16_t*)nullptr);
     else size((f16_t*)nullptr);
     LS_CHECK_LAUNCH();
     return LS_OK;
