@@ -276,8 +276,9 @@ template <int DH, int RW> constexpr int tree_lds() {
   return work > join ? work : join;
 }
 
+// head_dim 64 with rows of its own: three workgroups a compute unit (two: 24 nodes 49 us, 64 requests of 1024, 12 heads; three 39)
 template <class T, int DH, int NT, int RW>
-__global__ __launch_bounds__(256, 2) void tree_attn_kernel(const T* __restrict__ q, long ldq, T* __restrict__ o, long ldo,
+__global__ __launch_bounds__(256, DH == 64 && RW == 1 ? 3 : 2) void tree_attn_kernel(const T* __restrict__ q, long ldq, T* __restrict__ o, long ldo,
                                                            const T* __restrict__ k_pool, const T* __restrict__ v_pool,
                                                            const int32_t* __restrict__ table,
                                                            const uint64_t* __restrict__ masks, Tree tr, int h, int hk,
@@ -456,7 +457,8 @@ __global__ __launch_bounds__(256, 2) void tree_attn_kernel(const T* __restrict__
     const int k0 = t * KEYS;
     const bool plain = decltype(plain_)::value || is_plain(t, bad);
     // Operand of the second product: keys 4 quad + (col / 4), head dimensions 16 j + 4 (col % 4) ..: the lane receives its column
-    // of the 4 x 16 block.  Those of the first 32 keys are read behind the softmax, the others as registers come free.
+    // of the 4 x 16 block.  Those of the first 32 keys are read ahead of the softmax, the others as registers come free.
+    constexpr bool EARLY = !(RW == 1 && NT == 2);   // the other two sets of rows have no registers for them by then
     V8 vf[DT];
     int at = v_get;
     asm volatile("" : "+v"(at));
@@ -468,7 +470,7 @@ __global__ __launch_bounds__(256, 2) void tree_attn_kernel(const T* __restrict__
       vf[j] = __builtin_bit_cast(V8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
     };
 #pragma unroll
-    for (int j = 0; j < DT; ++j) read_v(0, j);
+    for (int j = 0; j < DT; ++j) if (EARLY) read_v(0, j);
     uint64_t seen[NT];   // bit r: the lane's row sees key k0 + r
     if (!plain) {
       uint64_t live = k_hi - k0 >= 64 ? ~0ull : (1ull << (k_hi - k0)) - 1;
@@ -487,7 +489,12 @@ __global__ __launch_bounds__(256, 2) void tree_attn_kernel(const T* __restrict__
             if (!(mine >> (16 * c + i) & 1)) sacc[n][c][i] = -INFINITY;
       }
     }
-    V8 pf[NT][H];
+    // The weights are the second product's operand, in 16 bits.  Where the bytes of K and V set the pace they come in two parts,
+    // rounded and remainder, and the product's error is that of its sums: rounded once, bf16 weights add as much to the result's
+    // error as its own rounding does.  Twice the products there cost nothing up to 16 rows and 2 % up to 32; with four wavefronts
+    // a tile, where the products count, 253 us would be 400, and each weight is rounded once, by half a step at most.
+    constexpr bool SPLIT = RW == 1;
+    V8 pf[NT][H], pl[SPLIT ? NT : 1][SPLIT ? H : 1];
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
       float mc[2 * H];
@@ -515,7 +522,9 @@ __global__ __launch_bounds__(256, 2) void tree_attn_kernel(const T* __restrict__
         for (int i = 0; i < 4; ++i) {
           const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(sacc[n][c][i], scale_log2, -ref));
           sacc[n][c][i] = p;
-          pf[n][c >> 1][4 * (c & 1) + i] = from_f<T>(p);   // the second product's operand: 16 bits, relative error of half a step each
+          const T hi = from_f<T>(p);
+          pf[n][c >> 1][4 * (c & 1) + i] = hi;
+          if constexpr (SPLIT) pl[n][c >> 1][4 * (c & 1) + i] = from_f<T>(p - to_f(hi));
         }
       float lc[2 * H];
 #pragma unroll
@@ -528,7 +537,11 @@ __global__ __launch_bounds__(256, 2) void tree_attn_kernel(const T* __restrict__
 #pragma unroll
       for (int j = 0; j < DT; ++j) {
 #pragma unroll
-        for (int n = 0; n < NT; ++n) oacc[n][j] = Mma16<T>::run(vf[j], pf[n][hf], oacc[n][j]);
+        for (int n = 0; n < NT; ++n) {
+          if (!EARLY && n == 0) read_v(0, j);
+          oacc[n][j] = Mma16<T>::run(vf[j], pf[n][hf], oacc[n][j]);
+          if constexpr (SPLIT) oacc[n][j] = Mma16<T>::run(vf[j], pl[n][hf], oacc[n][j]);
+        }
         if (hf + 1 < H) read_v(hf + 1, j);
       }
     if (!plain && odd) {
