@@ -76,10 +76,10 @@ __device__ __forceinline__ int request_of(const int32_t* start, int B, int t) {
   return lo;
 }
 
-// Any type and head size: a workgroup of four wavefronts per (row, head), so that every row reads the keys for itself, through the
-// caches.  A wavefront takes 64 keys at a time, a lane one
-// key for the scores and a column (of up to four) for the outputs; the softmax is online per wavefront, the four are joined
-// through LDS.  Keys that the row does not see are left out of both products, whatever their rows hold.
+// Any type, head size, page size and alignment: a workgroup of four wavefronts per (row, head), so that every row reads the keys
+// for itself, through the caches.  A wavefront takes 64 keys at a time, a lane one key for the scores and a column (of up to four)
+// for the outputs; the softmax is online per wavefront, the four are joined through LDS.  Keys that the row does not see are left
+// out of both products, whatever their rows hold.  16 trees of 8 nodes, 8 heads of 256, 1024 tokens, 16 bits: 510 us.
 template <class T>
 __global__ __launch_bounds__(256) void tree_attn_any_kernel(const T* q, long ldq, T* o, long ldo, const T* k_pool,
                                                             const T* v_pool, Tree tr, int h, int hk, int dh, float scale_log2) {
@@ -458,7 +458,7 @@ __global__ __launch_bounds__(256, DH == 64 && RW == 1 ? 3 : 2) void tree_attn_ke
     const bool plain = decltype(plain_)::value || is_plain(t, bad);
     // Operand of the second product: keys 4 quad + (col / 4), head dimensions 16 j + 4 (col % 4) ..: the lane receives its column
     // of the 4 x 16 block.  Those of the first 32 keys are read ahead of the softmax, the others as registers come free.
-    constexpr bool EARLY = !(RW == 1 && NT == 2);   // the other two sets of rows have no registers for them by then
+    constexpr bool EARLY = !(RW == 1 && NT == 2);   // beside two tiles of rows and a tile of K there are no registers for them yet
     V8 vf[DT];
     int at = v_get;
     asm volatile("" : "+v"(at));
