@@ -101,7 +101,8 @@ int ls_server_in_flight(const ls_server* sv);
  * ls_pages_grow     gives a row pages for n_tokens tokens, of which written_from .. n_tokens - 1 are about to be written: pages
  *                   of these that other rows hold too are replaced by free ones.  Where such a page also holds tokens before
  *                   written_from, its copy is asked for in src / dst (capacity max_pages_per_row, at most one in fact).  A row
- *                   that is long enough already keeps its length.  LS_ENOMEM, and nothing changed, without enough free pages.
+ *                   that is long enough already keeps its pages; what it held from token n_tokens on counts as given up, as
+ *                   tokens behind a rewritten one are.  LS_ENOMEM, and nothing changed, without enough free pages.
  * ls_pages_fork     gives row `to`, which has no pages, the pages of the first n_tokens tokens of row `from`: nothing is copied
  *                   until one of the two grows into a shared page.
  * ls_pages_truncate returns the pages past n_tokens tokens (0: all of them; a rejected draft, a finished request); a page is

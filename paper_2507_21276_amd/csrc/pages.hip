@@ -87,7 +87,7 @@ ls_status ls_pages_grow(ls_pages* p, int row, int written_from, int n_tokens, in
   const long need = ((long)n_tokens + p->page - 1) / p->page;
   LS_REQUIRE(need <= p->max_pages, "pages_grow: %d tokens need %ld pages, a row holds %d", n_tokens, need, p->max_pages);
   int32_t* ids = p->table.data() + (size_t)row * p->max_pages;
-  const int have = p->count[row], first = written_from / p->page;
+  const int have = p->count[row], first = written_from < n_tokens ? written_from / p->page : have;   // nothing written: none shared
   // pages that tokens written_from .. n_tokens - 1 lie on
   long fresh = need > have ? need - have : 0;
   for (int j = first; j < have && j < need; ++j) fresh += p->users[ids[j]] > 1;

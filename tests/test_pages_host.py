@@ -76,6 +76,14 @@ def test_pages_that_are_written_anew_are_not_copied():
     m.check()
 
 
+def test_growing_by_nothing_leaves_shared_pages_shared():
+    p = sched.Pages(3, 8, 2, 3)
+    assert p.grow(0, 0, 20) == ([], [])
+    p.fork(0, 1, 20)
+    for at in (0, 5, 16, 20):                    # no token is written, so no page is asked for: there is none left
+        assert p.grow(1, at, at) == ([], []) and p.row(1) == p.row(0) == [0, 1, 2]
+
+
 def test_compaction_fills_the_lowest_pages():
     m = Model(12, 4, 4, 6)
     for row in range(4):
