@@ -254,6 +254,7 @@ class KV:
         kv = cls.__new__(cls)
         kv.stage, kv.k_pool, kv.v_pool, kv.n_pages = None, k_pool, v_pool, k_pool.shape[1]
         assert k_pool.is_contiguous() and v_pool.is_contiguous() and k_pool.shape == v_pool.shape
+        assert block_table is None or block_table.dtype is torch.int32
         kv.block_table = None if block_table is None else block_table.contiguous()
         kv.ctx_host = kv.ctx_len = None
         if ctx_len is not None:
@@ -626,6 +627,16 @@ def _here(t, stream):
     return torch._C._cuda_getCurrentRawStream(dev) if stream is None else _stream(stream)
 
 
+def _scratch(n, t, stream):
+    """n floats beside t for a call on that stream; not given out again before the call's work there has ended."""
+    s = torch.empty(n, dtype=torch.float32, device=t.device)
+    if stream is not None:
+        raw = _stream(stream) or 0
+        if raw != torch._C._cuda_getCurrentRawStream(t.get_device()):
+            s.record_stream(stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(raw, t.device))
+    return s
+
+
 def _at(t):
     """Pointer of a dense tensor, None for none."""
     if t is None:
@@ -690,8 +701,7 @@ def lsk_qk_norm_rope_bwd(dout, qkv, din, n_heads, n_kv_heads, head_dim, *, gain_
     if dgain_q is not None:
         assert dgain_k is not None and dgain_q.dtype is dgain_k.dtype is torch.float32, "both gradients of the gains, in fp32"
         assert dgain_q.numel() == head_dim == dgain_k.numel()
-        partial = torch.empty(L.lsk_qk_norm_rope_bwd_partial_floats(T, n_heads, n_kv_heads, head_dim), dtype=torch.float32,
-                              device=dout.device)
+        partial = _scratch(L.lsk_qk_norm_rope_bwd_partial_floats(T, n_heads, n_kv_heads, head_dim), dout, stream)
     _check(L.lsk_qk_norm_rope_bwd(*_rows(dout, T, width), *(_rows(qkv, T, width) if qkv is not None else (None, 0)),
                                   *_rows(din, T, width), CODE_OF_TORCH[dout.dtype], T, n_heads, n_kv_heads, head_dim,
                                   *_norm_rope(T, head_dim, gain_q, gain_k, norm, eps, pos, table, layout), _at(dgain_q), _at(dgain_k),
@@ -733,10 +743,11 @@ def lsk_attn_tree(q, o, n_heads, n_kv_heads, head_dim, start, ctx_len, mask, max
     T, B, dtype, L = q.shape[0], start.numel() - 1, q.dtype, lib()
     assert o.dtype is dtype and mask.shape == (T, (max_nodes + 63) // 64) and mask.element_size() == 8 and block_table.dtype is _INT
     kp, vp, n_pages = _pools(k_pool, v_pool, n_kv_heads, page_size, head_dim, dtype)
+    assert block_table.shape[0] >= B, "a row of page ids for each request"
     if scratch is None:
         n = L.lsk_attn_tree_scratch_floats(T, B, n_heads, n_kv_heads, head_dim, max_nodes, max_ctx)
         if n:
-            scratch = torch.empty(n, dtype=torch.float32, device=q.device)
+            scratch = _scratch(n, q, stream)
     else:
         n = scratch.numel()
         assert scratch.dtype is torch.float32
@@ -745,16 +756,27 @@ def lsk_attn_tree(q, o, n_heads, n_kv_heads, head_dim, start, ctx_len, mask, max
                            page_size, n_pages, max_ctx, *_rows(o, T, n_heads * head_dim), _at(scratch), n, _here(q, stream)))
 
 
+def _pool_of(config, kv):
+    """The descriptor of pools that are as large as the configuration says."""
+    d = kv.desc(False)
+    n = config.n_layers * d.n_pages * config.n_heads * config.page_size * config.head_dim
+    assert kv.k_pool.numel() == n == kv.v_pool.numel() and kv.k_pool.dtype is kv.v_pool.dtype is TORCH_DTYPE[config.mma_dtype], \
+        "pools of another configuration"
+    return d
+
+
 def lsk_kv_copy_pages(config, kv, src, dst, stream=None):
     """Pages src[i] -> dst[i] (host integers) of all layers; config: the pool's ls_config."""
     n = len(src)
     assert len(dst) == n
     ints = C.c_int32 * (n or 1)
-    _check(lib().lsk_kv_copy_pages(config, kv.desc(False), ints(*src), ints(*dst), n, _here(kv.k_pool, stream)))
+    _check(lib().lsk_kv_copy_pages(config, _pool_of(config, kv), ints(*src), ints(*dst), n, _here(kv.k_pool, stream)))
 
 
 def lsk_kv_move_rows(config, kv, path, n_path, stream=None):
     """Rows of the accepted nodes path [B, max_path] (n_path [B] of them) of every request to the end of its context."""
     B, most = path.shape
-    _check(lib().lsk_kv_move_rows(config, kv.desc(False), B, _indexes(path, B * most), most, _indexes(n_path, B),
+    assert kv.block_table is not None and kv.ctx_len is not None, "pools without a block table or lengths"
+    assert kv.block_table.shape[0] >= B <= kv.ctx_len.numel(), "a row of page ids and a length for each request"
+    _check(lib().lsk_kv_move_rows(config, _pool_of(config, kv), B, _indexes(path, B * most), most, _indexes(n_path, B),
                                   _here(path, stream)))

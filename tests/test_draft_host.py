@@ -3,6 +3,7 @@ import ctypes as C
 
 import numpy as np
 import pytest
+import torch
 
 from paper_2507_21276_amd import binding as Bd
 
@@ -168,3 +169,27 @@ def test_stage_verify_validates_its_arguments_before_any_launch():
     assert call() == Bd.LS_EINVAL and "negative" in err()
     assert call(kv=Bd.ls_kv(P, P, None, P, None, 8, 3)) == Bd.LS_EINVAL and "null field" in err()
     lib.ls_destroy(h)
+
+
+def test_wrappers_refuse_tables_and_pools_that_are_too_small():
+    """Tensors on the CPU: each call is refused before anything looks at the device."""
+    z = lambda *n, t=torch.int32: torch.zeros(*n, dtype=t)  # noqa: E731
+    q, pool, mask = z(4, 128, t=torch.float16), z(8, 2, 16, 64, t=torch.float16), z(4, 1, t=torch.int64)
+    with pytest.raises(AssertionError, match="page ids"):
+        Bd.lsk_attn_tree(q, q.clone(), 2, 2, 64, z(4), z(3), mask, 4, pool, pool, z(2, 4), 16, 30)
+    pools, c = z(2, 8, 2, 16, 64, t=torch.bfloat16), pool_config(mma_dtype="bf16")
+    path, n_path = z(3, 4), z(3)
+    with pytest.raises(AssertionError, match="page ids"):
+        Bd.lsk_kv_move_rows(c, Bd.KV.of(pools, pools, z(2, 4), [0, 0, 0]), path, n_path)
+    with pytest.raises(AssertionError, match="without"):
+        Bd.lsk_kv_move_rows(c, Bd.KV.of(pools, pools, z(3, 4)), path, n_path)
+    with pytest.raises(AssertionError, match="length"):
+        Bd.lsk_kv_move_rows(c, Bd.KV.of(pools, pools, z(3, 4), [0, 0]), path, n_path)
+    kv = Bd.KV.of(pools, pools, z(3, 4), [0, 0, 0])
+    for other in (dict(n_layers=3), dict(page_size=32), dict(n_heads=4, d_model=256), dict(mma_dtype="f16")):
+        with pytest.raises(AssertionError, match="another configuration"):
+            Bd.lsk_kv_move_rows(pool_config(**{"mma_dtype": "bf16", **other}), kv, path, n_path)
+        with pytest.raises(AssertionError, match="another configuration"):
+            Bd.lsk_kv_copy_pages(pool_config(**{"mma_dtype": "bf16", **other}), kv, [0], [1])
+    with pytest.raises(AssertionError):
+        Bd.KV.of(pools, pools, z(3, 4, t=torch.int64))

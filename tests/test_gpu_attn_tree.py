@@ -315,3 +315,23 @@ def test_captured_calls_on_other_streams():
             c.run(q=x, o=y, scratch=z, **args)
     torch.cuda.synchronize()
     assert all(torch.equal(a, b) for a, b in zip(outs, wants))
+
+
+def test_scratch_of_a_call_on_a_stream_that_is_not_the_current_one():
+    """The wrapper's own scratch is not handed to the current stream's work while the call has yet to run on its own."""
+    c = Case(15, [1500, 90], [12, 5], 4, 2, 128, 16, "f16")
+    args = [i32(c.start), i32(c.past), c.mask(), c.max_nodes, c.kp.cuda(), c.vp.cuda(), i32(c.bt), 16, 1500]
+    q, o = c.q.cuda(), torch.empty(c.T, 512, dtype=torch.float16, device="cuda")
+    n = Bd.lib().lsk_attn_tree_scratch_floats(c.T, 2, 4, 2, 128, c.max_nodes, 1500)
+    assert n > 0
+    side = torch.cuda.Stream()
+    for stream in (side, side.cuda_stream):
+        o.fill_(7.0)
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            torch.cuda._sleep(2000000)
+        Bd.lsk_attn_tree(q, o, 4, 2, 128, *args, stream=stream)
+        others = [torch.full((n,), float("nan"), device="cuda") for _ in range(4)]
+        torch.cuda.synchronize()
+        c.check(o)
+        del others

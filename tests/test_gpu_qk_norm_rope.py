@@ -301,3 +301,22 @@ def test_a_captured_training_pass_replays():
         step(*e)
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(e, (out, dx, dgq, dgk)))
+
+
+def test_partial_sums_of_a_backward_on_a_stream_that_is_not_the_current_one():
+    T, h, hk, dh = 300, 4, 2, 128
+    c = case(29, T, h, hk, dh, dh, 0, "bf16", "f32")
+    x, dy = c["qkv"].cuda(), rand(50, c["qkv"].shape, "bf16").cuda()
+    n = Bd.lib().lsk_qk_norm_rope_bwd_partial_floats(T, h, hk, dh)
+    assert n > 0
+    want, got, dx = [torch.empty(dh, device="cuda") for _ in range(2)], [torch.empty(dh, device="cuda") for _ in range(2)], torch.empty_like(x)
+    Bd.lsk_qk_norm_rope_bwd(dy, x, dx, h, hk, dh, dgain_q=want[0], dgain_k=want[1], **c["kw"])
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(2000000)
+    Bd.lsk_qk_norm_rope_bwd(dy, x, dx, h, hk, dh, dgain_q=got[0], dgain_k=got[1], stream=side, **c["kw"])
+    others = [torch.full((n,), float("nan"), device="cuda") for _ in range(4)]
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(want, got))
+    del others
