@@ -153,9 +153,10 @@ __global__ __launch_bounds__(256) void tree_attn_any_kernel(const T* q, long ldq
 //   16384 tokens each: 6.7 TB/s; of 128 to 2048 tokens 5.9 (216 us; with K and V read through the caches 239; two register sets
 //   of a tile and spills 330).
 //   RW = 2, 4 (more rows): bound by the exponentials and the products.  K and V tiles are loaded once for the RW wavefronts,
-//   through two LDS buffers and one barrier a tile, of 64 keys where all four share it.  64 trees of 64 nodes, five query heads a
-//   key head, 16384 tokens each: 630 TFLOP/s; 12 of 40 - 61 nodes, 3000 to 16001 tokens: 480 (253 us; a wavefront with 64 rows of its
-//   own, which spills, 489; tiles of 32 keys 326).  The matrix cores are busy a third of the time, the vector units half.
+//   straight to two LDS buffers and with one barrier a tile, of 64 keys where all four share it.  12 trees of 40 - 61 nodes, five
+//   query heads a key head, 3000 to 16001 tokens: 510 TFLOP/s (238 us; by way of registers, which are 32 more, 254; a wavefront with
+//   64 rows of its own, which spills, 489; tiles of 32 keys 326); 64 of 64 nodes, 4096 tokens each, 467 us, by way of registers 500.
+//   No single part sets the pace: without the exponentials 228 us, without the loads 197, without the second product 206.
 template <class T> struct Mma16;
 template <> struct Mma16<bf16_t> {
   typedef bf16x8 V8;
@@ -272,7 +273,7 @@ __device__ __forceinline__ uint64_t window(const uint64_t* mask, int words, int 
 
 constexpr int tree_halves(int rw) { return rw == 4 ? 2 : 1; }   // of a tile, 32 keys each
 template <int DH, int RW> constexpr int tree_lds() {
-  constexpr int KW = 4 / RW, tile = tree_halves(RW) * 32 * DH * 2, work = RW == 1 ? 4 * tile : 2 * KW * 2 * tile, join = 4 * 16 * (DH + 4) * 4;
+  constexpr int KW = 4 / RW, tile = tree_halves(RW) * 32 * DH * 2, work = RW == 1 ? 4 * tile : KW * 2 * tile, join = 4 * 16 * (DH + 4) * 4;
   return work > join ? work : join;
 }
 
@@ -289,7 +290,9 @@ __global__ __launch_bounds__(256, DH == 64 && RW == 1 ? 3 : 2) void tree_attn_ke
   constexpr int NL = H * DH / 16 / RW;                      // loads of K, and of V, per wavefront and tile
   constexpr int G = 4 * H / RW;                             // groups of eight rows that a wavefront loads
   constexpr int TILE = KEYS * DH * 2;
+  // Two objects, so that the compiler knows that reads of one do not wait for the loads that go to the other
   __shared__ __attribute__((aligned(16))) char smem[tree_lds<DH, RW>()];
+  __shared__ __attribute__((aligned(16))) char smem2[RW == 1 ? 16 : KW * 2 * TILE];
   __shared__ float s_m[4][NT * 16], s_l[4][NT * 16];
   __shared__ int s_flag[2][KW][RW];   // of the tile in a buffer: groups of rows on no page, and values that are not finite
 
@@ -356,8 +359,8 @@ __global__ __launch_bounds__(256, DH == 64 && RW == 1 ? 3 : 2) void tree_attn_ke
     }
     return w;
   };
-  // loads of a tile in registers: K as the lane's operand of the first product (RW = 1) or in whole rows, V in whole rows
-  struct Set { V8 k[RW == 1 ? 2 * KS : NL], v[NL]; int bad; };
+  // loads of a tile in registers (RW = 1): K as the lane's operand of the first product, V in whole rows
+  struct Set { V8 k[2 * KS], v[NL]; int bad; };
   // Loads of whole rows: 64 lanes read 512 elements, 512 / DH rows, from one group of eight rows (head_dim 32: from two).  The
   // group's offset is the wavefront's, the lane's place in it 8 lane elements.
   auto row_of = [&](int j) { return (rw * NL + j) * (64 / LPR) + lane / LPR; };
@@ -371,22 +374,14 @@ __global__ __launch_bounds__(256, DH == 64 && RW == 1 ? 3 : 2) void tree_attn_ke
     }
   };
   // K and V that one workgroup reads are read past the caches
-  auto load = [&](const T* p) {
-    if constexpr (RW < 4) return __builtin_nontemporal_load((const V8*)p);
-    else return *(const V8*)p;
-  };
+  auto load = [&](const T* p) { return __builtin_nontemporal_load((const V8*)p); };
   auto fetch_k = [&](const Where& w, Set& set) {
-    if constexpr (RW == 1) {
 #pragma unroll
-      for (int c = 0; c < 2; ++c) {
-        const long a0 = w.at[2 * c], a1 = w.at[2 * c + 1];
-        const T* kr = k_pool + ((lane >> 3) & 1 ? a1 : a0) + (lane & 7) * DH + quad * 8;
+    for (int c = 0; c < 2; ++c) {
+      const long a0 = w.at[2 * c], a1 = w.at[2 * c + 1];
+      const T* kr = k_pool + ((lane >> 3) & 1 ? a1 : a0) + (lane & 7) * DH + quad * 8;
 #pragma unroll
-        for (int s = 0; s < KS; ++s) set.k[c * KS + s] = load(kr + s * 32);
-      }
-    } else {
-#pragma unroll
-      for (int j = 0; j < NL; ++j) set.k[j] = load(rows_at(k_pool, w, j));
+      for (int s = 0; s < KS; ++s) set.k[c * KS + s] = load(kr + s * 32);
     }
   };
   auto fetch_v = [&](const Where& w, Set& set) {
@@ -396,10 +391,9 @@ __global__ __launch_bounds__(256, DH == 64 && RW == 1 ? 3 : 2) void tree_attn_ke
   };
   // A lane's byte offsets in the tiles.  Both swizzles are an exclusive or of the piece with row bits that a load, a step of a
   // product or a half of the tile does not touch, or only as a constant: the other offsets follow from these.
-  const int v_put = v_at<DH>(lane / LPR, lane % LPR) + rw * NL * 1024, k_put = k_at<DH>(lane / LPR, lane % LPR) + rw * NL * 1024;
+  const int v_put = v_at<DH>(lane / LPR, lane % LPR) + rw * NL * 1024;
   const int v_get = v_at<DH>(4 * quad + (col >> 2), (col >> 1) & 1) + (col & 1) * 8, k_get = k_at<DH>(col, quad);
   auto v_put_at = [&](int j) { return (v_put ^ (DH == 128 ? (j & 1) << 7 : 0)) + j * 1024; };
-  auto k_put_at = [&](int j) { return (k_put ^ (DH == 128 ? (j & 3) << 6 : DH == 64 ? (j & 1) << 6 : 0)) + j * 1024; };
   auto is_plain = [&](int t, int bad) { return (t + 1) * KEYS <= ctx && (t + 1) * KEYS <= k_hi && bad == 0; };   // all rows see all keys
   // V to LDS.  In the tiles that some row does not see whole, values that are not finite are left out of the product (0 * x
   // would reach the rows that do not see them); returns whether there were any.
@@ -499,7 +493,7 @@ __global__ __launch_bounds__(256, DH == 64 && RW == 1 ? 3 : 2) void tree_attn_ke
     for (int n = 0; n < NT; ++n) {
       float mc[2 * H];
 #pragma unroll
-      for (int c = 0; c < 2 * H; ++c) mc[c] = fmaxf(fmaxf(sacc[n][c][0], sacc[n][c][1]), fmaxf(sacc[n][c][2], sacc[n][c][3]));
+      for (int c = 0; c < 2 * H; ++c) mc[c] = fmaxf(fmaxf(fmaxf(sacc[n][c][0], sacc[n][c][1]), sacc[n][c][2]), sacc[n][c][3]);
       float mx = fmaxf(mc[0], mc[1]);
       if constexpr (H == 2) mx = fmaxf(mx, fmaxf(mc[2], mc[3]));
       mx = quads_max(mx) * scale_log2;
@@ -612,45 +606,77 @@ __global__ __launch_bounds__(256, DH == 64 && RW == 1 ? 3 : 2) void tree_attn_ke
     bool gaps = false;
     for (int p = (k_lo >> shift) + threadIdx.x; p <= (k_hi - 1) >> shift; p += 256) gaps |= (unsigned)bt[p] >= (unsigned)tr.n_pages;
     const bool any_gap = __syncthreads_or(gaps);
-    // The loads of a tile are asked for as soon as the one before it is in LDS
-    Set set;
-    int t = t_lo + kw;
+    // Direct-to-LDS loads.  64 lanes write 1 KB one after the other, so a lane asks for the piece of its row that the swizzle puts
+    // in its place: element offsets in the rows of a load, to which a later load adds a constant.
+    const int k_lane = (lane / LPR) * DH + ((lane % LPR) ^ ((k_at<DH>(lane / LPR, 0) >> 4) & (LPR - 1))) * 8;
+    const int v_lane = (lane / LPR) * DH + ((lane % LPR) ^ ((v_at<DH>(lane / LPR, 0) >> 4) & (LPR - 1))) * 8;
+    constexpr int PAST = RW < 4 ? 2 : 0;   // past the caches where one workgroup reads the keys
+    auto issue = [&](char* st, const Where& w) {
+      char* kt = st + kw * 2 * TILE + rw * NL * 1024;
+#pragma unroll
+      for (int j = 0; j < NL; ++j) {
+        const int r = j * (64 / LPR);
+        long at;
+        if constexpr (DH == 32) at = lane < 32 ? w.at[r >> 3] : w.at[(r >> 3) + 1] - 8 * DH;   // lanes count on over the two groups
+        else at = w.at[r >> 3] + (r & 7) * DH;
+        const int kx = DH == 128 ? (j & 3) << 5 : DH == 64 ? (j & 1) << 5 : 0, vx = DH == 128 ? (j & 1) << 6 : 0;
+        const T *kp = k_pool + at + (k_lane ^ kx), *vp = v_pool + at + (v_lane ^ vx);
+        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)kp,
+                                         (__attribute__((address_space(3))) void*)(kt + j * 1024), 16, 0, PAST);
+        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)vp,
+                                         (__attribute__((address_space(3))) void*)(kt + TILE + j * 1024), 16, 0, PAST);
+      }
+    };
+    int t = t_lo + kw, i = t_lo, bad = 0;
     Ids ids = look_up(t);
     if (t < t_hi) {
       const Where w = find(t, ids);
-      fetch_v(w, set);
-      fetch_k(w, set);
+      bad = w.bad;
+      issue(smem, w);
     }
     ids = look_up(t + KW);
-    for (int i = t_lo, buf = 0; i < t_hi; i += KW, buf ^= 1, t += KW) {   // the same number of trips in every wavefront
-      char* kt = smem + (buf * KW + kw) * 2 * TILE;
+    // A tile of each set of wavefronts from `cur`, while the next one's loads go to `nxt`.  Waits are the compiler's own, so that it
+    // knows which loads are still under way: it would otherwise wait for `nxt` before it reads `cur`.
+    auto step = [&](char* cur, char* nxt, int buf) __attribute__((always_inline)) {
+      char* kt = cur + kw * 2 * TILE;
       char* vt = kt + TILE;
-      const Where next = find(t + KW, ids);   // of ids that came during the tile before this one: no wait behind the stores
-      if (t < t_hi) {
-        const bool odd = put_v(any_tile, vt, t, set);
+      const Where next = find(t + KW, ids);   // of ids that came during the tile before this one
+      const bool all = !any_gap && is_plain(t, 0);
+      asm volatile("" ::: "memory");
+      __builtin_amdgcn_s_waitcnt(0x0070);     // vmcnt(0), lgkmcnt(0): the wavefront's own loads are here
+      asm volatile("" ::: "memory");
+      if (!all && t < t_hi) {                 // its own rows of V once more through put_v
+        Set set;
+        set.bad = bad;
 #pragma unroll
-        for (int j = 0; j < NL; ++j) *(V8*)(kt + k_put_at(j)) = set.k[j];
-        if (lane == 0) s_flag[buf][kw][rw] = set.bad | (int)odd << 8;
+        for (int j = 0; j < NL; ++j) set.v[j] = *(const V8*)(vt + v_put_at(j));
+        const bool odd = put_v(any_tile, vt, t, set);
+        if (lane == 0) s_flag[buf][kw][rw] = bad | (int)odd << 8;
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_waitcnt(0x0070);
       }
-      if (t + KW < t_hi) {
-        fetch_v(next, set);
-        fetch_k(next, set);
-      }
+      __builtin_amdgcn_s_barrier();           // everyone's are, and everyone is past the tile before this one: `nxt` is free
+      asm volatile("" ::: "memory");
+      if (t + KW < t_hi) issue(nxt, next);
+      bad = next.bad;
       ids = look_up(t + 2 * KW);
-      // all are past the tile before this one: its buffer is the next to be written
-      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
-      __builtin_amdgcn_s_barrier();
-      __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
       if (t < t_hi && row0 < rows) {
         int flags = 0;
-        if (any_gap || !is_plain(t, 0)) {
+        if (!all) {
 #pragma unroll
           for (int w = 0; w < RW; ++w) flags |= s_flag[buf][kw][w];
           flags = __builtin_amdgcn_readfirstlane(flags);
         }
-        first_product(kt, set);
+        first_product(kt, Set());
         attend(any_tile, vt, t, flags & 255, flags >> 8);
       }
+      t += KW;
+      i += KW;
+    };
+    while (i < t_hi) {   // the same number of trips in every wavefront
+      step(smem, smem2, 0);
+      if (i >= t_hi) break;
+      step(smem2, smem, 1);
     }
   }
   store_rows<T, DH, NT, RW>(oacc, m_run, l_run, smem, s_m, s_l, Rows{first, rows, rb * ROWS, kvh, g, h, used, part}, parts, o, ldo);
