@@ -617,7 +617,7 @@ def lsk_finish_qkv(partial, splits, n_heads, head_dim, pos, req, table, qkv, k_p
 #
 # These calls are small next to a projection: what the host does per call is kept short, and each shape is looked at once.
 
-_INT = torch.int32
+_INT, _F32 = torch.int32, torch.float32
 
 
 def _here(t, stream):
@@ -662,17 +662,28 @@ def _indexes(t, n):
 
 def _norm_rope(T, head_dim, gain_q, gain_k, norm, eps, pos, table, layout):
     """The arguments that the forms of lsk_qk_norm_rope share, from kind on."""
-    gain = gain_q if gain_q is not None else gain_k
-    code = 0
-    if gain is not None:
-        code = CODE_OF_TORCH[gain.dtype]
-        assert gain.numel() == head_dim and (gain_k is None or (gain_k.numel() == head_dim and gain_k.dtype is gain.dtype))
-    rot = n_pos = 0
+    gq = gk = ps = tb = None
+    code = rot = n_pos = 0
+    if gain_q is not None or gain_k is not None:
+        gain = gain_q if gain_q is not None else gain_k
+        dtype = gain.dtype
+        code = CODE_OF_TORCH[dtype]
+        if gain_q is not None:
+            assert gain_q.numel() == head_dim and gain_q.is_contiguous()
+            gq = gain_q.data_ptr()
+        if gain_k is not None:
+            assert gain_k.dtype is dtype and gain_k.numel() == head_dim and gain_k.is_contiguous()
+            gk = gain_k.data_ptr()
     if table is not None:
         n_pos, half, two = table.shape
         rot = 2 * half
-        assert two == 2 and table.dtype is torch.float32 and pos is not None, "an fp32 table of cos and sin needs positions"
-    return 1 if norm else -1, _at(gain_q), _at(gain_k), code, eps, rot, layout, _indexes(pos, T), _at(table), n_pos
+        assert two == 2 and table.dtype is _F32 and pos is not None and table.is_contiguous(), \
+            "a dense fp32 table of cos and sin needs positions"
+        tb = table.data_ptr()
+    if pos is not None:
+        assert pos.dtype is _INT and pos.numel() >= T and pos.is_contiguous(), "dense 32-bit integers, one a row"
+        ps = pos.data_ptr()
+    return 1 if norm else -1, gq, gk, code, eps, rot, layout, ps, tb, n_pos
 
 
 def lsk_rope_table(table, theta, scaling=None, stream=None):
@@ -708,25 +719,29 @@ def lsk_qk_norm_rope_bwd(dout, qkv, din, n_heads, n_kv_heads, head_dim, *, gain_
                                   1 if accumulate else 0, _at(alpha), _at(partial), _here(dout, stream)))
 
 
-def _pools(k_pool, v_pool, n_kv_heads, page_size, head_dim, dtype):
-    """Pointers of the pools and the number of their pages."""
+def _same_pools(k_pool, v_pool, page, dtype):
+    """Whether both pools are dense and of pages of that shape and type."""
     shape = k_pool.shape
-    assert shape == v_pool.shape and shape[1:] == (n_kv_heads, page_size, head_dim) and k_pool.dtype is v_pool.dtype is dtype
-    return _at(k_pool), _at(v_pool), shape[0]
+    return (shape == v_pool.shape and shape[1:] == page and k_pool.dtype is dtype and v_pool.dtype is dtype
+            and k_pool.is_contiguous() and v_pool.is_contiguous())
 
 
 def lsk_qk_norm_rope_kv_write(qkv, q_out, n_heads, n_kv_heads, head_dim, pos, req, k_pool, v_pool, block_table, page_size, *,
                               slot=None, gain_q=None, gain_k=None, norm=True, eps=1e-5, table=None, layout=LSK_ROPE_HALF,
                               stream=None):
     """q of qkv, normalised and rotated, to q_out; k and v to their slots of the pools [n_pages, n_kv_heads, page, head_dim]."""
-    T, dtype = qkv.shape[0], qkv.dtype
-    assert q_out.dtype is dtype and block_table.dtype is _INT
-    kp, vp, n_pages = _pools(k_pool, v_pool, n_kv_heads, page_size, head_dim, dtype)
-    _check(lib().lsk_qk_norm_rope_kv_write(*_rows(qkv, T, (n_heads + 2 * n_kv_heads) * head_dim), *_rows(q_out, T, n_heads * head_dim),
-                                           CODE_OF_TORCH[dtype], T, n_heads, n_kv_heads, head_dim,
-                                           *_norm_rope(T, head_dim, gain_q, gain_k, norm, eps, pos, table, layout),
-                                           _indexes(req, T), _indexes(slot, T), kp, vp, _at(block_table), block_table.shape[1],
-                                           page_size, n_pages, _here(qkv, stream)))
+    (T, w), (ld, one) = qkv.shape, qkv.stride()
+    (T_q, w_q), (ld_q, one_q) = q_out.shape, q_out.stride()
+    dtype = qkv.dtype
+    assert T == T_q and one == 1 == one_q and w >= (n_heads + 2 * n_kv_heads) * head_dim and w_q >= n_heads * head_dim, \
+        "rows must be dense and wide enough"
+    assert q_out.dtype is dtype and _same_pools(k_pool, v_pool, (n_kv_heads, page_size, head_dim), dtype)
+    assert block_table.dtype is _INT and block_table.is_contiguous()
+    _check(lib().lsk_qk_norm_rope_kv_write(
+        qkv.data_ptr(), ld if T > 1 else w, q_out.data_ptr(), ld_q if T > 1 else w_q, CODE_OF_TORCH[dtype], T, n_heads, n_kv_heads,
+        head_dim, *_norm_rope(T, head_dim, gain_q, gain_k, norm, eps, pos, table, layout), _indexes(req, T), _indexes(slot, T),
+        k_pool.data_ptr(), v_pool.data_ptr(), block_table.data_ptr(), block_table.shape[1], page_size, k_pool.shape[0],
+        _here(qkv, stream)))
 
 
 def lsk_tree_index(parent, start, ctx_len, max_nodes, pos, slot, req, mask, stream=None):
@@ -740,20 +755,27 @@ def lsk_tree_index(parent, start, ctx_len, max_nodes, pos, slot, req, mask, stre
 def lsk_attn_tree(q, o, n_heads, n_kv_heads, head_dim, start, ctx_len, mask, max_nodes, k_pool, v_pool, block_table, page_size,
                   max_ctx, scratch=None, stream=None):
     """o [T, n_heads head_dim] of the drafted trees' rows q over the pools [n_pages, n_kv_heads, page, head_dim]."""
-    T, B, dtype, L = q.shape[0], start.numel() - 1, q.dtype, lib()
-    assert o.dtype is dtype and mask.shape == (T, (max_nodes + 63) // 64) and mask.element_size() == 8 and block_table.dtype is _INT
-    kp, vp, n_pages = _pools(k_pool, v_pool, n_kv_heads, page_size, head_dim, dtype)
-    assert block_table.shape[0] >= B, "a row of page ids for each request"
+    (T, w), (ld, one) = q.shape, q.stride()
+    (T_o, w_o), (ld_o, one_o) = o.shape, o.stride()
+    n_rows, per_row = block_table.shape
+    B, dtype, L, at = start.numel() - 1, q.dtype, lib(), None
+    assert T == T_o and one == 1 == one_o and w >= n_heads * head_dim <= w_o, "rows must be dense and wide enough"
+    assert o.dtype is dtype and _same_pools(k_pool, v_pool, (n_kv_heads, page_size, head_dim), dtype)
+    assert mask.shape == (T, (max_nodes + 63) // 64) and mask.element_size() == 8 and mask.is_contiguous()
+    assert n_rows >= B and block_table.dtype is _INT and block_table.is_contiguous(), "a row of page ids for each request"
     if scratch is None:
         n = L.lsk_attn_tree_scratch_floats(T, B, n_heads, n_kv_heads, head_dim, max_nodes, max_ctx)
         if n:
             scratch = _scratch(n, q, stream)
+            at = scratch.data_ptr()
     else:
         n = scratch.numel()
-        assert scratch.dtype is torch.float32
-    _check(L.lsk_attn_tree(*_rows(q, T, n_heads * head_dim), CODE_OF_TORCH[dtype], T, B, max_nodes, n_heads, n_kv_heads, head_dim,
-                           _indexes(start, 2), _indexes(ctx_len, B), _at(mask), kp, vp, _at(block_table), block_table.shape[1],
-                           page_size, n_pages, max_ctx, *_rows(o, T, n_heads * head_dim), _at(scratch), n, _here(q, stream)))
+        assert scratch.dtype is _F32 and scratch.is_contiguous()
+        at = scratch.data_ptr()
+    _check(L.lsk_attn_tree(
+        q.data_ptr(), ld if T > 1 else w, CODE_OF_TORCH[dtype], T, B, max_nodes, n_heads, n_kv_heads, head_dim, _indexes(start, 2),
+        _indexes(ctx_len, B), mask.data_ptr(), k_pool.data_ptr(), v_pool.data_ptr(), block_table.data_ptr(), per_row, page_size,
+        k_pool.shape[0], max_ctx, o.data_ptr(), ld_o if T > 1 else w_o, at, n, _here(q, stream)))
 
 
 def _pool_of(config, kv):
