@@ -63,6 +63,7 @@ struct Tree {
   int B, T, max_nodes, words;
   const int32_t* block_table;
   int max_pages, page, n_pages;
+  int order_bit;   // the requests' order is that of their lengths in this bit and the five below it; -1: as they come
 };
 
 // The request of row t: the last one whose first row is not behind it
@@ -150,11 +151,11 @@ __global__ __launch_bounds__(256) void tree_attn_any_kernel(const T* q, long ldq
 // keys, which two transposing LDS reads per 16 head dimensions do.
 //   RW = 1 (up to 32 rows): bound by the K and V bytes.  Each is loaded by one wavefront; K goes straight to registers as the
 //   first product's operand, V to the wavefront's own LDS buffer: no barrier in the loop.  64 trees of 8 nodes, 32 heads of 128,
-//   16384 tokens each: 6.7 TB/s; of 128 to 2048 tokens 5.9 (216 us; with K and V read through the caches 239; two register sets
-//   of a tile and spills 330).
+//   16384 tokens each: 6.7 TB/s; of 128 to 2048 tokens 6.6 (194 us; the requests as they come 216, with K and V read through the caches as
+//   well 239; two register sets of a tile and spills 330).
 //   RW = 2, 4 (more rows): bound by the exponentials and the products.  K and V tiles are loaded once for the RW wavefronts,
 //   straight to two LDS buffers and with one barrier a tile, of 64 keys where all four share it.  12 trees of 40 - 61 nodes, five
-//   query heads a key head, 3000 to 16001 tokens: 510 TFLOP/s (238 us; by way of registers, which are 32 more, 254; a wavefront with
+//   query heads a key head, 3000 to 16001 tokens: 520 TFLOP/s (234 us; by way of registers, which are 32 more, 254; a wavefront with
 //   64 rows of its own, which spills, 489; tiles of 32 keys 326); 64 of 64 nodes, 4096 tokens each, 467 us, by way of registers 500.
 //   No single part sets the pace: without the exponentials 228 us, without the loads 197, without the second product 206.
 template <class T> struct Mma16;
@@ -262,6 +263,28 @@ __device__ __forceinline__ void store_rows(const f32x4 (&oacc)[NT][DH / 16], con
   }
 }
 
+// Workgroups that do not all fit on the chip at once take the requests of each 64 in falling order of their contexts, so that short
+// ones end the launch: bf16, 32 heads of 128, 128 to 2048 tokens, 64 trees of 8 nodes 190 -> 172 us, 32 of 13 115 -> 101.  Every
+// wavefront finds its own: one load, then bit by bit of the length the half in which the place-th longest lies; among equal ones
+// the order is theirs.
+__device__ __forceinline__ int request_at(const Tree& tr, int place) {
+  if (tr.order_bit < 0) return place;
+  const int base = place & ~63, n = min(64, tr.B - base), lane = threadIdx.x & 63;
+  const int len = tr.ctx_len[base + min(lane, n - 1)];
+  uint64_t left = n == 64 ? ~0ull : (1ull << n) - 1;
+  int k = place & 63;   // of those left
+#pragma unroll
+  for (int i = 0; i < 6; ++i) {
+    if (tr.order_bit < i) break;
+    const uint64_t longer = __builtin_amdgcn_ballot_w64(len >> (tr.order_bit - i) & 1) & left;
+    const int c = __popcll(longer);
+    if (k < c) left = longer;
+    else { left &= ~longer; k -= c; }
+  }
+  const int before = __builtin_amdgcn_mbcnt_hi((uint32_t)(left >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)left, 0));
+  return base + __ffsll((unsigned long long)__builtin_amdgcn_ballot_w64((left >> lane & 1) && before == k)) - 1;
+}
+
 // Bits of 64 nodes from node nd0 on of a mask row: whether the row sees the key that lies there.  Below 0 lie cached tokens.
 __device__ __forceinline__ uint64_t window(const uint64_t* mask, int words, int nd0) {
   const int w0 = nd0 >> 6, sh = nd0 & 63;
@@ -299,7 +322,7 @@ __global__ __launch_bounds__(256, DH == 64 && RW == 1 ? 3 : 2) void tree_attn_ke
   // Blocks of rows that read the same keys follow each other on one XCD (workgroups go round the eight of them)
   const int slot8 = blockIdx.x >> 3, item = (slot8 / parts.row_blocks) * 8 + (blockIdx.x & 7), rb = slot8 % parts.row_blocks;
   if (item >= tr.B * hk) return;
-  const int b = item / hk, kvh = item % hk, part = blockIdx.y, g = h / hk;
+  const int b = request_at(tr, item / hk), kvh = item % hk, part = blockIdx.y, g = h / hk;
   const int first = tr.start[b], nodes = min(min(tr.start[b + 1], tr.T) - first, tr.max_nodes), rows = nodes * g;
   if (first < 0 || rb * ROWS >= rows) return;
   const int ctx = max(tr.ctx_len[b], 0), page = 1 << shift;
@@ -700,7 +723,7 @@ __global__ __launch_bounds__(256, 2) void tree_attn_f32_kernel(const float* __re
   __shared__ float s_m[4][NT * 16], s_l[4][NT * 16];
   const int slot8 = blockIdx.x >> 3, item = (slot8 / parts.row_blocks) * 8 + (blockIdx.x & 7), rb = slot8 % parts.row_blocks;
   if (item >= tr.B * hk) return;
-  const int b = item / hk, kvh = item % hk, part = blockIdx.y, g = h / hk;
+  const int b = request_at(tr, item / hk), kvh = item % hk, part = blockIdx.y, g = h / hk;
   const int first = tr.start[b], nodes = min(min(tr.start[b + 1], tr.T) - first, tr.max_nodes), rows = nodes * g;
   if (first < 0 || rb * ROWS >= rows) return;
   const int ctx = max(tr.ctx_len[b], 0), page = 1 << shift;
@@ -980,7 +1003,7 @@ ls_status lsk_attn_tree(const void* q, long ldq, int dt, int T, int B, int max_n
   LS_REQUIRE(dh > 0 && dh <= 256, "attn_tree: head_dim %d outside 1..256", dh);
   LS_REQUIRE(max_nodes > 0 && max_nodes <= kMaxNodes, "attn_tree: max_nodes %d outside 1..%d", max_nodes, kMaxNodes);
   LS_REQUIRE(ldq >= (long)h * dh && ldo >= (long)h * dh, "attn_tree: rows overlap (ldq %ld, ldo %ld)", ldq, ldo);
-  const Tree tr = {start, ctx_len, mask, B, T, max_nodes, (max_nodes + 63) / 64, block_table, max_pages, page, n_pages};
+  Tree tr = {start, ctx_len, mask, B, T, max_nodes, (max_nodes + 63) / 64, block_table, max_pages, page, n_pages, -1};
   const float scale_log2 = 1.4426950408889634f / sqrtf((float)dh);
   hipStream_t st = (hipStream_t)stream;
   const int per16 = dt == LS_F32 ? 4 : 8;   // elements of 16 bytes
@@ -996,6 +1019,7 @@ ls_status lsk_attn_tree(const void* q, long ldq, int dt, int T, int B, int max_n
     const long groups = ((long)B * hk + 7) / 8 * 8 * p.row_blocks;
     LS_REQUIRE(groups <= 0x7fffffffL, "attn_tree: too many (request, head) pairs");
     const dim3 grid((unsigned)groups, p.parts);
+    if (B > 1 && max_ctx > 0 && groups * p.parts > 512) tr.order_bit = 31 - __builtin_clz(max_ctx);   // two workgroups a compute unit
     const int shift = __builtin_ctz(page);
     const long merge = ((long)max_nodes * h + 3) / 4;   // workgroups a request
     LS_REQUIRE(merge * B <= 0x7fffffffL, "attn_tree: too many (row, head) pairs");

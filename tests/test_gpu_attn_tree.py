@@ -335,3 +335,19 @@ def test_scratch_of_a_call_on_a_stream_that_is_not_the_current_one():
         torch.cuda.synchronize()
         c.check(o)
         del others
+
+
+# more workgroups than the chip holds at once, whose requests go by length: equal and empty contexts, more than 64 requests, a
+# last group of a few, shared key heads and parts
+@pytest.mark.parametrize("dtype,B,lo,hi,n,h,hk,dh", [("f16", 131, 0, 40, 2, 4, 4, 64), ("bf16", 65, 0, 3, 40, 10, 10, 32), ("f16", 66, 0, 90, 70, 8, 8, 128),
+                                                     ("f32", 129, 5, 9, 3, 5, 5, 32), ("bf16", 17, 100, 1500, 30, 16, 8, 64),
+                                                     ("f32", 3, 0, 3000, 9, 64, 64, 32), ("f16", 600, 0, 4, 1, 1, 1, 128)])
+def test_many_requests_of_different_lengths(dtype, B, lo, hi, n, h, hk, dh):
+    rng = np.random.default_rng(16)
+    past, counts = [int(v) for v in rng.integers(lo, hi + 1, B)], [int(v) for v in rng.integers(0, n + 1, B)]
+    counts[B // 2] = n
+    c = Case(17, past, counts, h, hk, dh, 16, dtype)
+    scratch = torch.empty(max(1, Bd.lib().lsk_attn_tree_scratch_floats(c.T, B, h, hk, dh, c.max_nodes, max(past))), device="cuda")
+    o = c.run(scratch=scratch)
+    c.check(o, rows=None if c.T * h < 4000 else set(rng.choice(c.T, 4000 // h, replace=False).tolist()))
+    assert not torch.isnan(o).any() and not (o == 7.0).all(1).any()      # every row was written
