@@ -352,13 +352,6 @@ __global__ __launch_bounds__(256, DH == 64 && RW == 1 ? 3 : 2) void tree_attn_ke
     for (int s = 0; s < KS; ++s) asm volatile("" : "+v"(qf[n][s]));
   f32x4 oacc[NT][DT];
   float m_run[NT], l_run[NT];
-#pragma unroll
-  for (int n = 0; n < NT; ++n) {
-    m_run[n] = -INFINITY;
-    l_run[n] = 0.f;
-#pragma unroll
-    for (int j = 0; j < DT; ++j) oacc[n][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-  }
 
   // A tile's rows lie in groups of eight on one page each: the ids of the pages of the wavefront's groups, read a tile before
   // they are needed, then the groups' offsets in the pools and which of them lie on no page (bits of the tile's groups)
@@ -417,7 +410,30 @@ __global__ __launch_bounds__(256, DH == 64 && RW == 1 ? 3 : 2) void tree_attn_ke
   const int v_put = v_at<DH>(lane / LPR, lane % LPR) + rw * NL * 1024;
   const int v_get = v_at<DH>(4 * quad + (col >> 2), (col >> 1) & 1) + (col & 1) * 8, k_get = k_at<DH>(col, quad);
   auto v_put_at = [&](int j) { return (v_put ^ (DH == 128 ? (j & 1) << 7 : 0)) + j * 1024; };
-  auto is_plain = [&](int t, int bad) { return (t + 1) * KEYS <= ctx && (t + 1) * KEYS <= k_hi && bad == 0; };   // all rows see all keys
+  // Tiles of which all rows see all keys are taken as they are.  There an infinite value times a weight that 16 bits do not hold, or
+  // times the remainder of one, is NaN where the weight itself, which is positive, gives infinity: results that are not finite are
+  // computed once more, with every tile looked through.  (Finite ones: 0 - 2 % for the registers that the way back takes.)
+  bool looked = false;
+  auto is_plain = [&](int t, int bad) { return !looked && (t + 1) * KEYS <= ctx && (t + 1) * KEYS <= k_hi && bad == 0; };
+  auto all_finite = [&] {
+    float x = 0.f;
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int j = 0; j < DT; ++j)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x = fmaf(oacc[n][j][i], 0.f, x);
+    return x == 0.f;
+  };
+  auto clear = [&] {
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      m_run[n] = -INFINITY;
+      l_run[n] = 0.f;
+#pragma unroll
+      for (int j = 0; j < DT; ++j) oacc[n][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+  };
   // V to LDS.  In the tiles that some row does not see whole, values that are not finite are left out of the product (0 * x
   // would reach the rows that do not see them); returns whether there were any.
   auto put_v = [&](auto plain_, char* vt, int t, const Set& set) {
@@ -602,8 +618,12 @@ __global__ __launch_bounds__(256, DH == 64 && RW == 1 ? 3 : 2) void tree_attn_ke
     // always has a tile in flight.  The tiles that every row sees whole come first; from the first other one on (behind the
     // context, or on a page that is not there) a second loop takes them all, so that its registers are not the first one's.
     char* vt = smem + wave * TILE;
-    int t = t_lo + wave;
-    if (t < t_hi) {
+    for (;;) {
+      clear();
+      int t = t_lo;
+      asm volatile("" : "+s"(t));   // made anew the second time: held over the loop, the first tile's offsets are registers that spill
+      t += wave;
+      if (t >= t_hi) break;
       Set set;
       Where next = find(t, look_up(t));
       fetch_v(next, set);
@@ -623,6 +643,8 @@ __global__ __launch_bounds__(256, DH == 64 && RW == 1 ? 3 : 2) void tree_attn_ke
       };
       while (t < t_hi && is_plain(t, set.bad)) step(plain_tile);
       while (t < t_hi) step(any_tile);
+      if (looked || __builtin_amdgcn_ballot_w64(!all_finite()) == 0) break;
+      looked = true;
     }
   } else {
     // whether any page of this part is not there: the flags of plain tiles are not looked at otherwise
@@ -650,14 +672,8 @@ __global__ __launch_bounds__(256, DH == 64 && RW == 1 ? 3 : 2) void tree_attn_ke
                                          (__attribute__((address_space(3))) void*)(kt + TILE + j * 1024), 16, 0, PAST);
       }
     };
-    int t = t_lo + kw, i = t_lo, bad = 0;
-    Ids ids = look_up(t);
-    if (t < t_hi) {
-      const Where w = find(t, ids);
-      bad = w.bad;
-      issue(smem, w);
-    }
-    ids = look_up(t + KW);
+    int t, bad;
+    Ids ids;
     // A tile of each set of wavefronts from `cur`, while the next one's loads go to `nxt`.  Waits are the compiler's own, so that it
     // knows which loads are still under way: it would otherwise wait for `nxt` before it reads `cur`.
     auto step = [&](char* cur, char* nxt, int buf) __attribute__((always_inline)) {
@@ -694,12 +710,27 @@ __global__ __launch_bounds__(256, DH == 64 && RW == 1 ? 3 : 2) void tree_attn_ke
         attend(any_tile, vt, t, flags & 255, flags >> 8);
       }
       t += KW;
-      i += KW;
     };
-    while (i < t_hi) {   // the same number of trips in every wavefront
-      step(smem, smem2, 0);
-      if (i >= t_hi) break;
-      step(smem2, smem, 1);
+    for (;;) {
+      clear();
+      t = t_lo;
+      asm volatile("" : "+s"(t));
+      t += kw;
+      bad = 0;
+      ids = look_up(t);
+      if (t < t_hi) {
+        const Where w = find(t, ids);
+        bad = w.bad;
+        issue(smem, w);
+      }
+      ids = look_up(t + KW);
+      for (int i = t_lo; i < t_hi; i += KW) {   // the same number of trips in every wavefront
+        step(smem, smem2, 0);
+        if ((i += KW) >= t_hi) break;
+        step(smem2, smem, 1);
+      }
+      if (looked || !__syncthreads_or(!all_finite())) break;
+      looked = true;
     }
   }
   store_rows<T, DH, NT, RW>(oacc, m_run, l_run, smem, s_m, s_l, Rows{first, rows, rb * ROWS, kvh, g, h, used, part}, parts, o, ldo);

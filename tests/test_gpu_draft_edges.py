@@ -1,0 +1,45 @@
+"""The drafted-token calls at their edges: values that are not finite and pages that are not there in every form of the tree
+attention's work, sizes beyond one launch, arrays and streams other than the usual ones."""
+import numpy as np
+import pytest
+import torch
+
+import draft_util as D
+from paper_2507_21276_amd import binding as Bd
+from test_gpu_attn_tree import DT, Case, f64, i32
+
+pytestmark = pytest.mark.gpu
+
+# (nodes, heads, key heads): 8 and 24 rows of a key head are a wavefront's own, 50 are shared by two, 160 by four
+ROWS = [(8, 1, 1), (24, 1, 1), (25, 2, 1), (40, 4, 1)]
+
+
+@pytest.mark.parametrize("value", [float("inf"), -float("inf")])
+@pytest.mark.parametrize("nodes,h,hk", ROWS)
+@pytest.mark.parametrize("dtype,dh", [("f16", 64), ("bf16", 64), ("f16", 128), ("bf16", 128), ("bf16", 32), ("f32", 64), ("f16", 80)])
+def test_an_infinite_value_of_the_context_reaches_every_row(dtype, dh, nodes, h, hk, value):
+    """Cached tokens are seen by all rows: an infinity in one of their values is the result there, whatever its weight
+    (e^-30: less than 16 bits hold beside 1), and the other dimensions do not notice."""
+    for key, weight, scratch in ((0, 0.0, None), (333, -30.0, None), (640, 0.0, torch.empty(0, device="cuda"))):
+        c = Case(21, [700], [nodes], h, hk, dh, 16, dtype)
+        c.q.view(-1, dh)[:, 0] = 8.0
+        page = c.bt[0]
+        for j in range(700 + nodes):
+            c.kp[page[j // 16], :, j % 16, 0] = weight * dh ** 0.5 / 8 if j == key else 0.0
+        at = page[key // 16], slice(None), key % 16, dh - 3
+        c.vp[at] = value
+        o = c.run(scratch=scratch).view(nodes, h, dh)
+        assert (o[..., dh - 3].float() == value).all()
+        c.vp[at] = 0.0
+        zero = c.run(scratch=scratch).view(nodes, h, dh)
+        o[..., dh - 3] = zero[..., dh - 3]
+        c.check(o.view(nodes, h * dh), set(range(0, nodes, 7)))
+
+
+@pytest.mark.parametrize("nodes,h,hk", ROWS)
+def test_infinities_of_both_signs_are_no_number(nodes, h, hk):
+    for dtype in ("f16", "bf16", "f32"):
+        c = Case(22, [300], [nodes], h, hk, 64, 16, dtype)
+        c.vp[c.bt[0, 1], :, 3, 5], c.vp[c.bt[0, 9], :, 8, 5] = float("inf"), -float("inf")
+        o = c.run().view(-1, 64).float()
+        assert torch.isnan(o[:, 5]).all() and torch.isfinite(o[:, :5]).all() and torch.isfinite(o[:, 6:]).all()
