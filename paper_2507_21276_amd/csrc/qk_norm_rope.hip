@@ -53,13 +53,17 @@ __device__ __forceinline__ const float* angles(const Shape& s, int t) {
 
 enum { OUT_ROWS = 0, IN_PLACE = 1, TO_PAGES = 2 };
 
+// Workgroups along x at most: a launch's work-items along one dimension are counted in 32 bits, and a larger grid wraps without
+// an error.  More workgroups go on along the next free dimension.
+constexpr long kGridX = 1 << 22;
+
 // Any even dh up to 512, any alignment: one wavefront per (row, head), a lane holds up to four pairs.  Two-byte accesses: a
 // quarter to a third of the vectorised kernels' rate.
 template <int LAYOUT, int MODE>
 __global__ __launch_bounds__(256) void norm_rope_any_kernel(const void* in, long ld_in, void* out, long ld_out, int dt, Shape s,
                                                             Pages pg) {
   const int heads = s.h + s.hk + (MODE == IN_PLACE ? 0 : s.hk);
-  const long item = (long)blockIdx.x * 4 + (threadIdx.x >> 6);
+  const long item = ((long)blockIdx.y * gridDim.x + blockIdx.x) * 4 + (threadIdx.x >> 6);
   const int lane = threadIdx.x & 63;
   if (item >= (long)s.T * heads) return;
   const int t = (int)(item / heads), hd = (int)(item % heads);
@@ -260,7 +264,7 @@ template <class T, int LAYOUT, int LPH, int MODE>
 __global__ __launch_bounds__(256) void norm_rope_kernel(const T* in, long ld_in, T* out, long ld_out, Shape s, Pages pg, int per) {
   typedef typename Four<T>::type V4;
   const int sub = threadIdx.x % LPH, grp = threadIdx.x / LPH;
-  const long t = (long)blockIdx.x * (256 / LPH / per) + grp / per;
+  const long t = ((long)blockIdx.z * gridDim.x + blockIdx.x) * (256 / LPH / per) + grp / per;
   if (t >= s.T) return;
   const int heads = s.h + s.hk + (MODE == IN_PLACE ? 0 : s.hk), first = grp % per + blockIdx.y * per * kHeads;
   if (first >= heads) return;
@@ -551,14 +555,15 @@ ls_status launch_fwd(const void* in, long ld_in, void* out, long ld_out, int dt,
       typedef std::remove_pointer_t<decltype(one)> T;
       constexpr int LPH = decltype(lph)::value, groups = 256 / LPH;
       const int need = pow2_from(heads), per = need < groups ? need : groups, tokens = groups / per;
-      const dim3 grid((unsigned)((s.T + tokens - 1) / tokens), (heads + per * kHeads - 1) / (per * kHeads));
+      const long n = ((long)s.T + tokens - 1) / tokens, x = n < kGridX ? n : kGridX;
+      const dim3 grid((unsigned)x, (heads + per * kHeads - 1) / (per * kHeads), (unsigned)((n + x - 1) / x));
       norm_rope_kernel<T, decltype(lay)::value, LPH, MODE><<<grid, 256, 0, st>>>((const T*)in, ld_in, (T*)out, ld_out, s, pg, per);
     });
     LS_CHECK_LAUNCH();
     return LS_OK;
   }
-  const long items = (long)s.T * heads;
-  const unsigned grid = (unsigned)((items + 3) / 4);
+  const long n = ((long)s.T * heads + 3) / 4, x = n < kGridX ? n : kGridX;
+  const dim3 grid((unsigned)x, (unsigned)((n + x - 1) / x));
   if (layout == LSK_ROPE_HALF) norm_rope_any_kernel<0, MODE><<<grid, 256, 0, st>>>(in, ld_in, out, ld_out, dt, s, pg);
   else norm_rope_any_kernel<1, MODE><<<grid, 256, 0, st>>>(in, ld_in, out, ld_out, dt, s, pg);
   LS_CHECK_LAUNCH();

@@ -43,3 +43,19 @@ def test_infinities_of_both_signs_are_no_number(nodes, h, hk):
         c.vp[c.bt[0, 1], :, 3, 5], c.vp[c.bt[0, 9], :, 8, 5] = float("inf"), -float("inf")
         o = c.run().view(-1, 64).float()
         assert torch.isnan(o[:, 5]).all() and torch.isfinite(o[:, :5]).all() and torch.isfinite(o[:, 6:]).all()
+
+
+@pytest.mark.parametrize("T,h,hk,dh", [((1 << 25) + 3, 1, 1, 2), ((1 << 28) + 5, 1, 1, 8)])
+def test_rows_of_more_workgroups_than_one_grid_dimension_counts(T, h, hk, dh):
+    """More than 2^32 work-items, in the kernel for any size and in the vectorised one: every row is written."""
+    x = torch.empty(T, (h + 2 * hk) * dh, dtype=torch.float16, device="cuda").random_(-2048, 2049)
+    y = torch.full_like(x, 7.0)
+    Bd.lsk_qk_norm_rope(x, y, h, hk, dh, norm=False)
+    assert torch.equal(x, y)
+    # in place, with a norm: the rows at both ends, around the border of the first grid row, and none left as it was
+    ends = torch.cat([torch.arange(9), torch.tensor([(1 << 24) - 1, 1 << 24, T // 2]), torch.arange(T - 9, T)]).cuda()
+    want = torch.empty_like(x[ends])
+    Bd.lsk_qk_norm_rope(x[ends].contiguous(), want, h, hk, dh)
+    Bd.lsk_qk_norm_rope(x, x, h, hk, dh)
+    assert torch.equal(x[ends], want)
+    assert float(x[:, :2 * dh].max()) <= dh ** 0.5 * (1 + D.HALF["f16"])
