@@ -9,6 +9,9 @@
 namespace {
 
 constexpr int kMaxNodes = 256;
+// Workgroups of 256 along x at most: a launch's work-items along one dimension are counted in 32 bits, and a larger grid wraps
+// without an error.
+constexpr long kGridX = (1 << 24) - 1;
 
 // pos, slot, request and ancestor mask of every node, from the parents: one workgroup per request, the last one marks the
 // rows behind the last tree.  A node's ancestors come before it, so a walk up the parents ends after at most its index.
@@ -1008,6 +1011,7 @@ ls_status lsk_tree_index(const int32_t* parent, const int32_t* start, const int3
   LS_REQUIRE(parent && start && ctx_len && pos && slot && req && mask, "tree_index: null argument");
   LS_REQUIRE(B > 0 && T > 0, "tree_index: non-positive size (B %d, T %d)", B, T);
   LS_REQUIRE(max_nodes > 0 && max_nodes <= kMaxNodes, "tree_index: max_nodes %d outside 1..%d", max_nodes, kMaxNodes);
+  LS_REQUIRE(B < kGridX, "tree_index: %d requests are too many", B);
   tree_index_kernel<<<(unsigned)B + 1, 256, 0, (hipStream_t)stream>>>(parent, start, ctx_len, B, T, max_nodes,
                                                                      (max_nodes + 63) / 64, pos, slot, req, mask);
   LS_CHECK_LAUNCH();
@@ -1044,16 +1048,16 @@ ls_status lsk_attn_tree(const void* q, long ldq, int dt, int T, int B, int max_n
     const size_t one = (size_t)T * h * (dh + 4);
     const size_t room = scratch && (uintptr_t)scratch % 16 == 0 ? scratch_floats / one : 0;
     if ((size_t)p.parts > room) p.parts = room > 1 ? (int)room : 1;
+    const long merge = ((long)max_nodes * h + 3) / 4;   // workgroups a request
+    if (merge * B > kGridX) p.parts = 1;                // nothing to join
     const long keys = (long)max_ctx + max_nodes;
     LS_REQUIRE(keys <= 0x7fffff00L, "attn_tree: max_ctx %d is too large", max_ctx);
     const Parts parts = {p.parts, part_keys(keys, p.parts), p.row_blocks, scratch};
     const long groups = ((long)B * hk + 7) / 8 * 8 * p.row_blocks;
-    LS_REQUIRE(groups <= 0x7fffffffL, "attn_tree: too many (request, head) pairs");
+    LS_REQUIRE(groups <= kGridX, "attn_tree: %d requests of up to %d nodes and %d key heads are too many", B, max_nodes, hk);
     const dim3 grid((unsigned)groups, p.parts);
     if (B > 1 && max_ctx > 0 && groups * p.parts > 512) tr.order_bit = 31 - __builtin_clz(max_ctx);   // two workgroups a compute unit
     const int shift = __builtin_ctz(page);
-    const long merge = ((long)max_nodes * h + 3) / 4;   // workgroups a request
-    LS_REQUIRE(merge * B <= 0x7fffffffL, "attn_tree: too many (row, head) pairs");
     auto go = [&](auto* one_, auto dh_, auto nt_, auto rw_) {
       typedef std::remove_pointer_t<decltype(one_)> T_;
       constexpr int DH = decltype(dh_)::value, NT = decltype(nt_)::value, RW = decltype(rw_)::value;
@@ -1089,6 +1093,7 @@ ls_status lsk_attn_tree(const void* q, long ldq, int dt, int T, int B, int max_n
     LS_CHECK_LAUNCH();
     return LS_OK;
   }
+  LS_REQUIRE(T <= kGridX, "attn_tree: %d rows are too many", T);
   auto any = [&](auto* one) {
     typedef std::remove_pointer_t<decltype(one)> T_;
     tree_attn_any_kernel<T_><<<dim3((unsigned)T, h), 256, 0, st>>>((const T_*)q, ldq, (T_*)o, ldo, (const T_*)k_pool,

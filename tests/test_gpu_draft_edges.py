@@ -59,3 +59,13 @@ def test_rows_of_more_workgroups_than_one_grid_dimension_counts(T, h, hk, dh):
     Bd.lsk_qk_norm_rope(x, x, h, hk, dh)
     assert torch.equal(x[ends], want)
     assert float(x[:, :2 * dh].max()) <= dh ** 0.5 * (1 + D.HALF["f16"])
+
+
+def test_contexts_stay_whole_where_the_join_would_be_too_large_a_launch():
+    """16384 requests of up to 256 nodes by 32 heads: a workgroup for each four (node, head) pairs of each is more than a launch
+    counts."""
+    B = 16384
+    past, counts = [0] * (B - 1) + [6500], [1] * (B - 2) + [256, 3]
+    c = Case(23, past, counts, 32, 1, 64, 16, "f16")
+    assert Bd.lib().lsk_attn_tree_scratch_floats(c.T, B, 32, 1, 64, 256, 6500) > 0
+    c.check(c.run(), {0, 5000, B - 3, B - 2, B + 100, c.T - 3, c.T - 1})
