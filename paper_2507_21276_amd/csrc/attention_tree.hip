@@ -2,6 +2,7 @@
 // verified by one forward).  The rows of a request are the nodes of its tree; their K and V rows lie in the pages behind the
 // ctx cached tokens, in node order, and node i attends to all cached tokens and to the nodes that its mask names (itself and
 // its ancestors).
+#include <algorithm>
 #include <type_traits>
 
 #include "common.h"
@@ -999,6 +1000,13 @@ Plan plan(int dt, int B, int hk, int g, int dh, int max_nodes, int max_ctx) {
   return p;
 }
 
+// What a call uses of its scratch at most, 1 GB: partial results grow with rows x heads x parts (4096 rows of 32 heads of 128 in
+// eight parts 554 MB, 16384 rows in 32 parts 8.9 GB), and fewer parts are right as well.  Launches that reach the limit have
+// thousands of workgroups, so that a split only shortens the last ones.
+constexpr size_t kMaxScratch = (size_t)1 << 28;   // floats
+
+bool mma_covers(int dh) { return dh == 32 || dh == 64 || dh == 128; }
+
 // keys of a part, for a context of the longest length: a whole number of tiles for each wavefront
 int part_keys(long keys, int parts) { return (int)(((keys + parts - 1) / parts + 127) / 128 * 128); }
 
@@ -1021,8 +1029,8 @@ ls_status lsk_tree_index(const int32_t* parent, const int32_t* start, const int3
 size_t lsk_attn_tree_scratch_floats(int T, int B, int h, int hk, int dh, int max_nodes, int max_ctx) {
   if (T <= 0 || B <= 0 || h <= 0 || hk <= 0 || h % hk || dh <= 0 || max_nodes <= 0 || max_ctx < 0) return 0;
   const int a = plan(LS_F32, B, hk, h / hk, dh, max_nodes, max_ctx).parts, b = plan(LS_F16, B, hk, h / hk, dh, max_nodes, max_ctx).parts;
-  const int parts = a > b ? a : b;
-  return parts > 1 ? (size_t)T * h * parts * (dh + 4) : 0;
+  const size_t one = (size_t)T * h * (dh + 4), parts = std::min<size_t>(a > b ? a : b, kMaxScratch / one);
+  return parts > 1 && mma_covers(dh) ? one * parts : 0;
 }
 
 ls_status lsk_attn_tree(const void* q, long ldq, int dt, int T, int B, int max_nodes, int h, int hk, int dh,
@@ -1042,11 +1050,11 @@ ls_status lsk_attn_tree(const void* q, long ldq, int dt, int T, int B, int max_n
   const float scale_log2 = 1.4426950408889634f / sqrtf((float)dh);
   hipStream_t st = (hipStream_t)stream;
   const int per16 = dt == LS_F32 ? 4 : 8;   // elements of 16 bytes
-  if ((dh == 32 || dh == 64 || dh == 128) && page >= 8 && (page & (page - 1)) == 0 && ldq % per16 == 0 && ldo % per16 == 0 &&
+  if (mma_covers(dh) && page >= 8 && (page & (page - 1)) == 0 && ldq % per16 == 0 && ldo % per16 == 0 &&
       ((uintptr_t)q | (uintptr_t)o | (uintptr_t)k_pool | (uintptr_t)v_pool) % 16 == 0) {
     Plan p = plan(dt, B, hk, h / hk, dh, max_nodes, max_ctx);
     const size_t one = (size_t)T * h * (dh + 4);
-    const size_t room = scratch && (uintptr_t)scratch % 16 == 0 ? scratch_floats / one : 0;
+    const size_t room = scratch && (uintptr_t)scratch % 16 == 0 ? std::min(scratch_floats, kMaxScratch) / one : 0;
     if ((size_t)p.parts > room) p.parts = room > 1 ? (int)room : 1;
     const long merge = ((long)max_nodes * h + 3) / 4;   // workgroups a request
     if (merge * B > kGridX) p.parts = 1;                // nothing to join
