@@ -254,6 +254,7 @@ class KV:
         kv = cls.__new__(cls)
         kv.stage, kv.k_pool, kv.v_pool, kv.n_pages = None, k_pool, v_pool, k_pool.shape[1]
         assert k_pool.is_contiguous() and v_pool.is_contiguous() and k_pool.shape == v_pool.shape
+        assert v_pool.device == k_pool.device and (block_table is None or block_table.device == k_pool.device), "on different devices"
         assert block_table is None or block_table.dtype is torch.int32
         kv.block_table = None if block_table is None else block_table.contiguous()
         kv.ctx_host = kv.ctx_len = None
@@ -620,9 +621,12 @@ def lsk_finish_qkv(partial, splits, n_heads, head_dim, pos, req, table, qkv, k_p
 _INT, _F32 = torch.int32, torch.float32
 
 
-def _here(t, stream):
-    """The stream of a call on t: t's device has to be the current one, and its current stream is the default."""
+def _here(stream, t, *others):
+    """The stream of a call on t and the other tensors (or None): all are on one GPU, the current one, whose current stream is
+    the default."""
     dev = t.get_device()
+    for x in others:
+        assert x is None or x.get_device() == dev, "tensors on different devices"
     assert dev == torch._C._cuda_getDevice(), "tensors on another device than the current one"
     return torch._C._cuda_getCurrentRawStream(dev) if stream is None else _stream(stream)
 
@@ -690,7 +694,7 @@ def lsk_rope_table(table, theta, scaling=None, stream=None):
     """Fills table [n_pos, rot_dim / 2, 2] with cos and sin."""
     n_pos, half, two = table.shape
     assert two == 2 and table.dtype is torch.float32
-    _check(lib().lsk_rope_table(_at(table), n_pos, 2 * half, theta, scaling, _here(table, stream)))
+    _check(lib().lsk_rope_table(_at(table), n_pos, 2 * half, theta, scaling, _here(stream, table)))
 
 
 def lsk_qk_norm_rope(qkv, out, n_heads, n_kv_heads, head_dim, *, gain_q=None, gain_k=None, norm=True, eps=1e-5, pos=None,
@@ -700,7 +704,7 @@ def lsk_qk_norm_rope(qkv, out, n_heads, n_kv_heads, head_dim, *, gain_q=None, ga
     assert qkv.dtype is out.dtype
     _check(lib().lsk_qk_norm_rope(*_rows(qkv, T, width), *_rows(out, T, width), CODE_OF_TORCH[qkv.dtype], T, n_heads, n_kv_heads,
                                   head_dim, *_norm_rope(T, head_dim, gain_q, gain_k, norm, eps, pos, table, layout),
-                                  _here(qkv, stream)))
+                                  _here(stream, qkv, out, gain_q, gain_k, pos, table)))
 
 
 def lsk_qk_norm_rope_bwd(dout, qkv, din, n_heads, n_kv_heads, head_dim, *, gain_q=None, gain_k=None, norm=True, eps=1e-5,
@@ -716,7 +720,8 @@ def lsk_qk_norm_rope_bwd(dout, qkv, din, n_heads, n_kv_heads, head_dim, *, gain_
     _check(L.lsk_qk_norm_rope_bwd(*_rows(dout, T, width), *(_rows(qkv, T, width) if qkv is not None else (None, 0)),
                                   *_rows(din, T, width), CODE_OF_TORCH[dout.dtype], T, n_heads, n_kv_heads, head_dim,
                                   *_norm_rope(T, head_dim, gain_q, gain_k, norm, eps, pos, table, layout), _at(dgain_q), _at(dgain_k),
-                                  1 if accumulate else 0, _at(alpha), _at(partial), _here(dout, stream)))
+                                  1 if accumulate else 0, _at(alpha), _at(partial),
+                                  _here(stream, dout, qkv, din, gain_q, gain_k, pos, table, dgain_q, dgain_k, alpha)))
 
 
 def _same_pools(k_pool, v_pool, page, dtype):
@@ -741,7 +746,7 @@ def lsk_qk_norm_rope_kv_write(qkv, q_out, n_heads, n_kv_heads, head_dim, pos, re
         qkv.data_ptr(), ld if T > 1 else w, q_out.data_ptr(), ld_q if T > 1 else w_q, CODE_OF_TORCH[dtype], T, n_heads, n_kv_heads,
         head_dim, *_norm_rope(T, head_dim, gain_q, gain_k, norm, eps, pos, table, layout), _indexes(req, T), _indexes(slot, T),
         k_pool.data_ptr(), v_pool.data_ptr(), block_table.data_ptr(), block_table.shape[1], page_size, k_pool.shape[0],
-        _here(qkv, stream)))
+        _here(stream, qkv, q_out, k_pool, v_pool, block_table, req, slot, gain_q, gain_k, pos, table)))
 
 
 def lsk_tree_index(parent, start, ctx_len, max_nodes, pos, slot, req, mask, stream=None):
@@ -749,7 +754,8 @@ def lsk_tree_index(parent, start, ctx_len, max_nodes, pos, slot, req, mask, stre
     T, B = pos.numel(), start.numel() - 1
     assert mask.shape == (T, (max_nodes + 63) // 64) and mask.element_size() == 8
     _check(lib().lsk_tree_index(_indexes(parent, T), _indexes(start, 2), _indexes(ctx_len, B), B, T, max_nodes, _indexes(pos, T),
-                                _indexes(slot, T), _indexes(req, T), _at(mask), _here(pos, stream)))
+                                _indexes(slot, T), _indexes(req, T), _at(mask),
+                                _here(stream, pos, parent, start, ctx_len, slot, req, mask)))
 
 
 def lsk_attn_tree(q, o, n_heads, n_kv_heads, head_dim, start, ctx_len, mask, max_nodes, k_pool, v_pool, block_table, page_size,
@@ -763,19 +769,21 @@ def lsk_attn_tree(q, o, n_heads, n_kv_heads, head_dim, start, ctx_len, mask, max
     assert o.dtype is dtype and _same_pools(k_pool, v_pool, (n_kv_heads, page_size, head_dim), dtype)
     assert mask.shape == (T, (max_nodes + 63) // 64) and mask.element_size() == 8 and mask.is_contiguous()
     assert n_rows >= B and block_table.dtype is _INT and block_table.is_contiguous(), "a row of page ids for each request"
-    if scratch is None:
+    n = 0
+    if scratch is not None:
+        n = scratch.numel()
+        assert scratch.dtype is _F32 and scratch.is_contiguous()
+        at = scratch.data_ptr()
+    elif max_ctx + max_nodes > 512:   # a call of fewer keys does not split a context
         n = L.lsk_attn_tree_scratch_floats(T, B, n_heads, n_kv_heads, head_dim, max_nodes, max_ctx)
         if n:
             scratch = _scratch(n, q, stream)
             at = scratch.data_ptr()
-    else:
-        n = scratch.numel()
-        assert scratch.dtype is _F32 and scratch.is_contiguous()
-        at = scratch.data_ptr()
     _check(L.lsk_attn_tree(
         q.data_ptr(), ld if T > 1 else w, CODE_OF_TORCH[dtype], T, B, max_nodes, n_heads, n_kv_heads, head_dim, _indexes(start, 2),
         _indexes(ctx_len, B), mask.data_ptr(), k_pool.data_ptr(), v_pool.data_ptr(), block_table.data_ptr(), per_row, page_size,
-        k_pool.shape[0], max_ctx, o.data_ptr(), ld_o if T > 1 else w_o, at, n, _here(q, stream)))
+        k_pool.shape[0], max_ctx, o.data_ptr(), ld_o if T > 1 else w_o, at, n,
+        _here(stream, q, o, start, ctx_len, mask, k_pool, v_pool, block_table, scratch)))
 
 
 def _pool_of(config, kv):
@@ -792,7 +800,7 @@ def lsk_kv_copy_pages(config, kv, src, dst, stream=None):
     n = len(src)
     assert len(dst) == n
     ints = C.c_int32 * (n or 1)
-    _check(lib().lsk_kv_copy_pages(config, _pool_of(config, kv), ints(*src), ints(*dst), n, _here(kv.k_pool, stream)))
+    _check(lib().lsk_kv_copy_pages(config, _pool_of(config, kv), ints(*src), ints(*dst), n, _here(stream, kv.k_pool, kv.v_pool)))
 
 
 def lsk_kv_move_rows(config, kv, path, n_path, stream=None):
@@ -801,4 +809,4 @@ def lsk_kv_move_rows(config, kv, path, n_path, stream=None):
     assert kv.block_table is not None and kv.ctx_len is not None, "pools without a block table or lengths"
     assert kv.block_table.shape[0] >= B <= kv.ctx_len.numel(), "a row of page ids and a length for each request"
     _check(lib().lsk_kv_move_rows(config, _pool_of(config, kv), B, _indexes(path, B * most), most, _indexes(n_path, B),
-                                  _here(path, stream)))
+                                  _here(stream, path, n_path, kv.k_pool, kv.v_pool, kv.block_table, kv.ctx_len)))
