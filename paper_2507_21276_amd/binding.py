@@ -632,13 +632,13 @@ def _here(stream, t, *others):
 
 
 def _scratch(n, t, stream):
-    """n floats beside t for a call on that stream; not given out again before the call's work there has ended."""
-    s = torch.empty(n, dtype=torch.float32, device=t.device)
-    if stream is not None:
-        raw = _stream(stream) or 0
-        if raw != torch._C._cuda_getCurrentRawStream(t.get_device()):
-            s.record_stream(stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(raw, t.device))
-    return s
+    """n floats beside t for a call on that stream.  They are the stream's own: a block of the current stream's could still be in
+    use by that stream's earlier work, which this one does not wait for, and could go to its later work too soon."""
+    raw = None if stream is None else _stream(stream) or 0
+    if raw is None or raw == torch._C._cuda_getCurrentRawStream(t.get_device()):
+        return torch.empty(n, dtype=torch.float32, device=t.device)
+    with torch.cuda.stream(stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(raw, t.device)):
+        return torch.empty(n, dtype=torch.float32, device=t.device)
 
 
 def _at(t):

@@ -69,3 +69,27 @@ def test_contexts_stay_whole_where_the_join_would_be_too_large_a_launch():
     c = Case(23, past, counts, 32, 1, 64, 16, "f16")
     assert Bd.lib().lsk_attn_tree_scratch_floats(c.T, B, 32, 1, 64, 256, 6500) > 0
     c.check(c.run(), {0, 5000, B - 3, B - 2, B + 100, c.T - 3, c.T - 1})
+
+
+def test_scratch_of_another_stream_is_no_block_of_the_current_one():
+    """A block that the current stream's work may still be using is not given to a call on another stream, and the call's own goes
+    back to its stream."""
+    n, t, side = 3 << 20, torch.empty(1, device="cuda"), torch.cuda.Stream()
+    for stream in (side, side.cuda_stream):
+        torch.cuda.synchronize()
+        block = torch.empty(n, device="cuda")
+        at = block.data_ptr()
+        del block                                    # free for the current stream, on which work with it may be pending
+        s = Bd._scratch(n, t, stream)
+        assert s.data_ptr() != at and s.numel() == n and s.dtype is torch.float32
+        mine = s.data_ptr()
+        del s
+        later = [torch.empty(n, device="cuda") for _ in range(3)]
+        assert mine not in [x.data_ptr() for x in later]
+        assert Bd._scratch(n, t, stream).data_ptr() == mine
+        del later
+    # the current stream's own: its blocks in turn
+    s = Bd._scratch(n, t, None)
+    at = s.data_ptr()
+    del s
+    assert Bd._scratch(n, t, torch.cuda.current_stream()).data_ptr() == at
