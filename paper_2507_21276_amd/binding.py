@@ -621,12 +621,16 @@ def lsk_finish_qkv(partial, splits, n_heads, head_dim, pos, req, table, qkv, k_p
 _INT, _F32 = torch.int32, torch.float32
 
 
-def _here(stream, t, *others):
-    """The stream of a call on t and the other tensors (or None): all are on one GPU, the current one, whose current stream is
-    the default."""
+def _device(t, *others):
+    """The device of t, which the other tensors (or None) are on as well."""
     dev = t.get_device()
     for x in others:
         assert x is None or x.get_device() == dev, "tensors on different devices"
+    return dev
+
+
+def _here(stream, dev):
+    """The stream of a call on tensors of that device, which has to be the current one: its current stream is the default."""
     assert dev == torch._C._cuda_getDevice(), "tensors on another device than the current one"
     return torch._C._cuda_getCurrentRawStream(dev) if stream is None else _stream(stream)
 
@@ -664,8 +668,8 @@ def _indexes(t, n):
     return t.data_ptr()
 
 
-def _norm_rope(T, head_dim, gain_q, gain_k, norm, eps, pos, table, layout):
-    """The arguments that the forms of lsk_qk_norm_rope share, from kind on."""
+def _norm_rope(dev, T, head_dim, gain_q, gain_k, norm, eps, pos, table, layout):
+    """The arguments that the forms of lsk_qk_norm_rope share, from kind on; the tensors are on the device dev."""
     gq = gk = ps = tb = None
     code = rot = n_pos = 0
     if gain_q is not None or gain_k is not None:
@@ -674,18 +678,22 @@ def _norm_rope(T, head_dim, gain_q, gain_k, norm, eps, pos, table, layout):
         code = CODE_OF_TORCH[dtype]
         if gain_q is not None:
             assert gain_q.numel() == head_dim and gain_q.is_contiguous()
+            assert gain_q.get_device() == dev, "tensors on different devices"
             gq = gain_q.data_ptr()
         if gain_k is not None:
             assert gain_k.dtype is dtype and gain_k.numel() == head_dim and gain_k.is_contiguous()
+            assert gain_k.get_device() == dev, "tensors on different devices"
             gk = gain_k.data_ptr()
     if table is not None:
         n_pos, half, two = table.shape
         rot = 2 * half
         assert two == 2 and table.dtype is _F32 and pos is not None and table.is_contiguous(), \
             "a dense fp32 table of cos and sin needs positions"
+        assert table.get_device() == dev, "tensors on different devices"
         tb = table.data_ptr()
     if pos is not None:
         assert pos.dtype is _INT and pos.numel() >= T and pos.is_contiguous(), "dense 32-bit integers, one a row"
+        assert pos.get_device() == dev, "tensors on different devices"
         ps = pos.data_ptr()
     return 1 if norm else -1, gq, gk, code, eps, rot, layout, ps, tb, n_pos
 
@@ -694,17 +702,17 @@ def lsk_rope_table(table, theta, scaling=None, stream=None):
     """Fills table [n_pos, rot_dim / 2, 2] with cos and sin."""
     n_pos, half, two = table.shape
     assert two == 2 and table.dtype is torch.float32
-    _check(lib().lsk_rope_table(_at(table), n_pos, 2 * half, theta, scaling, _here(stream, table)))
+    _check(lib().lsk_rope_table(_at(table), n_pos, 2 * half, theta, scaling, _here(stream, table.get_device())))
 
 
 def lsk_qk_norm_rope(qkv, out, n_heads, n_kv_heads, head_dim, *, gain_q=None, gain_k=None, norm=True, eps=1e-5, pos=None,
                      table=None, layout=LSK_ROPE_HALF, stream=None):
     """out = norm and rotation of q and k, and v, of qkv [T, (n_heads + 2 n_kv_heads) head_dim]; table [.., rot_dim / 2, 2]."""
-    T, width = qkv.shape[0], (n_heads + 2 * n_kv_heads) * head_dim
+    T, width, dev = qkv.shape[0], (n_heads + 2 * n_kv_heads) * head_dim, _device(qkv, out)
     assert qkv.dtype is out.dtype
     _check(lib().lsk_qk_norm_rope(*_rows(qkv, T, width), *_rows(out, T, width), CODE_OF_TORCH[qkv.dtype], T, n_heads, n_kv_heads,
-                                  head_dim, *_norm_rope(T, head_dim, gain_q, gain_k, norm, eps, pos, table, layout),
-                                  _here(stream, qkv, out, gain_q, gain_k, pos, table)))
+                                  head_dim, *_norm_rope(dev, T, head_dim, gain_q, gain_k, norm, eps, pos, table, layout),
+                                  _here(stream, dev)))
 
 
 def lsk_qk_norm_rope_bwd(dout, qkv, din, n_heads, n_kv_heads, head_dim, *, gain_q=None, gain_k=None, norm=True, eps=1e-5,
@@ -712,6 +720,7 @@ def lsk_qk_norm_rope_bwd(dout, qkv, din, n_heads, n_kv_heads, head_dim, *, gain_
                          stream=None):
     """din from dout and the forward's input; dgain_q, dgain_k (fp32, both or neither) (+)= alpha * the gains' gradients."""
     T, width, L, partial = dout.shape[0], (n_heads + 2 * n_kv_heads) * head_dim, lib(), None
+    dev = _device(dout, qkv, din, dgain_q, dgain_k, alpha)
     assert dout.dtype is din.dtype and (qkv is None or qkv.dtype is dout.dtype)
     if dgain_q is not None:
         assert dgain_k is not None and dgain_q.dtype is dgain_k.dtype is torch.float32, "both gradients of the gains, in fp32"
@@ -719,9 +728,8 @@ def lsk_qk_norm_rope_bwd(dout, qkv, din, n_heads, n_kv_heads, head_dim, *, gain_
         partial = _scratch(L.lsk_qk_norm_rope_bwd_partial_floats(T, n_heads, n_kv_heads, head_dim), dout, stream)
     _check(L.lsk_qk_norm_rope_bwd(*_rows(dout, T, width), *(_rows(qkv, T, width) if qkv is not None else (None, 0)),
                                   *_rows(din, T, width), CODE_OF_TORCH[dout.dtype], T, n_heads, n_kv_heads, head_dim,
-                                  *_norm_rope(T, head_dim, gain_q, gain_k, norm, eps, pos, table, layout), _at(dgain_q), _at(dgain_k),
-                                  1 if accumulate else 0, _at(alpha), _at(partial),
-                                  _here(stream, dout, qkv, din, gain_q, gain_k, pos, table, dgain_q, dgain_k, alpha)))
+                                  *_norm_rope(dev, T, head_dim, gain_q, gain_k, norm, eps, pos, table, layout), _at(dgain_q),
+                                  _at(dgain_k), 1 if accumulate else 0, _at(alpha), _at(partial), _here(stream, dev)))
 
 
 def _same_pools(k_pool, v_pool, page, dtype):
@@ -742,11 +750,14 @@ def lsk_qk_norm_rope_kv_write(qkv, q_out, n_heads, n_kv_heads, head_dim, pos, re
         "rows must be dense and wide enough"
     assert q_out.dtype is dtype and _same_pools(k_pool, v_pool, (n_kv_heads, page_size, head_dim), dtype)
     assert block_table.dtype is _INT and block_table.is_contiguous()
+    dev = qkv.get_device()
+    assert q_out.get_device() == dev == k_pool.get_device() and v_pool.get_device() == dev == block_table.get_device() \
+        and req.get_device() == dev and (slot is None or slot.get_device() == dev), "tensors on different devices"
     _check(lib().lsk_qk_norm_rope_kv_write(
         qkv.data_ptr(), ld if T > 1 else w, q_out.data_ptr(), ld_q if T > 1 else w_q, CODE_OF_TORCH[dtype], T, n_heads, n_kv_heads,
-        head_dim, *_norm_rope(T, head_dim, gain_q, gain_k, norm, eps, pos, table, layout), _indexes(req, T), _indexes(slot, T),
+        head_dim, *_norm_rope(dev, T, head_dim, gain_q, gain_k, norm, eps, pos, table, layout), _indexes(req, T), _indexes(slot, T),
         k_pool.data_ptr(), v_pool.data_ptr(), block_table.data_ptr(), block_table.shape[1], page_size, k_pool.shape[0],
-        _here(stream, qkv, q_out, k_pool, v_pool, block_table, req, slot, gain_q, gain_k, pos, table)))
+        _here(stream, dev)))
 
 
 def lsk_tree_index(parent, start, ctx_len, max_nodes, pos, slot, req, mask, stream=None):
@@ -755,7 +766,7 @@ def lsk_tree_index(parent, start, ctx_len, max_nodes, pos, slot, req, mask, stre
     assert mask.shape == (T, (max_nodes + 63) // 64) and mask.element_size() == 8
     _check(lib().lsk_tree_index(_indexes(parent, T), _indexes(start, 2), _indexes(ctx_len, B), B, T, max_nodes, _indexes(pos, T),
                                 _indexes(slot, T), _indexes(req, T), _at(mask),
-                                _here(stream, pos, parent, start, ctx_len, slot, req, mask)))
+                                _here(stream, _device(pos, parent, start, ctx_len, slot, req, mask))))
 
 
 def lsk_attn_tree(q, o, n_heads, n_kv_heads, head_dim, start, ctx_len, mask, max_nodes, k_pool, v_pool, block_table, page_size,
@@ -769,10 +780,14 @@ def lsk_attn_tree(q, o, n_heads, n_kv_heads, head_dim, start, ctx_len, mask, max
     assert o.dtype is dtype and _same_pools(k_pool, v_pool, (n_kv_heads, page_size, head_dim), dtype)
     assert mask.shape == (T, (max_nodes + 63) // 64) and mask.element_size() == 8 and mask.is_contiguous()
     assert n_rows >= B and block_table.dtype is _INT and block_table.is_contiguous(), "a row of page ids for each request"
+    dev = q.get_device()
+    assert o.get_device() == dev == start.get_device() and ctx_len.get_device() == dev == mask.get_device() \
+        and k_pool.get_device() == dev == v_pool.get_device() and block_table.get_device() == dev, "tensors on different devices"
     n = 0
     if scratch is not None:
         n = scratch.numel()
         assert scratch.dtype is _F32 and scratch.is_contiguous()
+        assert scratch.get_device() == dev, "tensors on different devices"
         at = scratch.data_ptr()
     elif max_ctx + max_nodes > 512:   # a call of fewer keys does not split a context
         n = L.lsk_attn_tree_scratch_floats(T, B, n_heads, n_kv_heads, head_dim, max_nodes, max_ctx)
@@ -783,7 +798,7 @@ def lsk_attn_tree(q, o, n_heads, n_kv_heads, head_dim, start, ctx_len, mask, max
         q.data_ptr(), ld if T > 1 else w, CODE_OF_TORCH[dtype], T, B, max_nodes, n_heads, n_kv_heads, head_dim, _indexes(start, 2),
         _indexes(ctx_len, B), mask.data_ptr(), k_pool.data_ptr(), v_pool.data_ptr(), block_table.data_ptr(), per_row, page_size,
         k_pool.shape[0], max_ctx, o.data_ptr(), ld_o if T > 1 else w_o, at, n,
-        _here(stream, q, o, start, ctx_len, mask, k_pool, v_pool, block_table, scratch)))
+        _here(stream, dev)))
 
 
 def _pool_of(config, kv):
@@ -800,7 +815,8 @@ def lsk_kv_copy_pages(config, kv, src, dst, stream=None):
     n = len(src)
     assert len(dst) == n
     ints = C.c_int32 * (n or 1)
-    _check(lib().lsk_kv_copy_pages(config, _pool_of(config, kv), ints(*src), ints(*dst), n, _here(stream, kv.k_pool, kv.v_pool)))
+    _check(lib().lsk_kv_copy_pages(config, _pool_of(config, kv), ints(*src), ints(*dst), n,
+                                   _here(stream, _device(kv.k_pool, kv.v_pool))))
 
 
 def lsk_kv_move_rows(config, kv, path, n_path, stream=None):
@@ -809,4 +825,4 @@ def lsk_kv_move_rows(config, kv, path, n_path, stream=None):
     assert kv.block_table is not None and kv.ctx_len is not None, "pools without a block table or lengths"
     assert kv.block_table.shape[0] >= B <= kv.ctx_len.numel(), "a row of page ids and a length for each request"
     _check(lib().lsk_kv_move_rows(config, _pool_of(config, kv), B, _indexes(path, B * most), most, _indexes(n_path, B),
-                                  _here(stream, path, n_path, kv.k_pool, kv.v_pool, kv.block_table, kv.ctx_len)))
+                                  _here(stream, _device(path, n_path, kv.k_pool, kv.v_pool, kv.block_table, kv.ctx_len))))
