@@ -331,9 +331,14 @@ class Stage:
         _check(lib().stage_decode(self.h, _p(X), B, C.byref(d), _p(Y), _p(workspace), _stream(stream)))
 
     def stage_verify(self, X, parent, start, n_nodes, kv: KV, Y, workspace, stream=None, with_host=True):
-        n = (C.c_int32 * max(1, len(n_nodes)))(*[int(v) for v in n_nodes])
+        """X, Y [T, d]; parent [T] and start [B + 1] (32-bit integers on the device) of trees of n_nodes [B] (host integers) rows."""
+        B, T = len(n_nodes), sum(n_nodes)
+        n = (C.c_int32 * max(1, B))(*[int(v) for v in n_nodes])
+        for x in (X, Y):
+            assert x is None or x.dtype is self.io_torch and x.numel() >= T * self.c.d_model, "rows of the stage's io type, one a node"
+        assert kv.block_table.shape[0] >= B <= kv.ctx_len.numel(), "a row of page ids and a length for each request"
         d = kv.desc(with_host)
-        _check(lib().stage_verify(self.h, _p(X), _p(parent), _p(start), n, len(n_nodes), C.byref(d), _p(Y), _p(workspace),
+        _check(lib().stage_verify(self.h, _p(X), _indexes(parent, T), _indexes(start, B + 1), n, B, C.byref(d), _p(Y), _p(workspace),
                                   _stream(stream)))
 
     def stage_train_fwd(self, X, B, L, Y, saved, workspace, stream=None):

@@ -144,3 +144,26 @@ def test_pools_tables_and_paths_lie_on_one_device(host_calls):
     with pytest.raises(AssertionError, match="device"):
         Bd.lsk_kv_copy_pages(cfg, kv, [0], [1])
     assert len(host_calls) == 2
+
+
+def test_stage_verify_looks_at_its_arrays(host_calls):
+    """Parents of another type, arrays shorter than the trees and a table of fewer rows: refused before the library reads them."""
+    class Small:
+        h, io_torch = None, torch.float32
+
+        class c:
+            d_model = 16
+
+    pool = z(1, 8, 1, 16, 16, t=torch.bfloat16)
+
+    def call(X=z(5, 16, **F32), parent=z(5), start=z(3), n=(2, 3), table=z(2, 4), ctx=(0, 0), Y=z(5, 16, **F32)):
+        Bd.Stage.stage_verify(Small(), X, parent, start, n, Bd.KV.of(pool, pool, table, ctx), Y, z(64), stream=0)
+
+    call()
+    assert host_calls == ["stage_verify"]
+    for over, text in ((dict(parent=z(5, t=torch.int64)), "32-bit"), (dict(parent=z(4)), "32-bit"), (dict(start=z(3, t=torch.int64)), "32-bit"),
+                       (dict(start=z(2)), "32-bit"), (dict(X=z(4, 16, **F32)), "io type"), (dict(Y=z(5, 15, **F32)), "io type"),
+                       (dict(X=z(5, 16, t=torch.bfloat16)), "io type"), (dict(table=z(1, 4)), "page ids"), (dict(ctx=(0,)), "length")):
+        with pytest.raises(AssertionError, match=text):
+            call(**over)
+    assert len(host_calls) == 1
