@@ -113,7 +113,7 @@ ls_status lsk_qk_norm_rope(const void* in, long ld_in, void* out, long ld_out, i
 /*
  * Backward of the above: din (rows of q | k | v) from dout and the forward's input `in` (may be null for kind -1).  din may
  * be dout (equal ld; v stays), must not overlap it otherwise and never overlaps `in`.  dgain_q, dgain_k [dev] fp32
- * [head_dim], both or neither (null): (accumulate ? old : 0) + alpha * the gains' gradients, summed over rows and heads in
+ * [head_dim], two arrays or neither (null): (accumulate ? old : 0) + alpha * the gains' gradients, summed over rows and heads in
  * a fixed order; alpha_dev [dev] as in the *_scaled calls (null = 1).  partial [dev]: fp32 scratch of
  * lsk_qk_norm_rope_bwd_partial_floats(T, n_heads, n_kv_heads, head_dim) elements (null without dgain_q).
  */

@@ -660,6 +660,7 @@ ls_status lsk_qk_norm_rope_bwd(const void* dout, long ld_dout, const void* in, l
   LS_REQUIRE(!dgain_q == !dgain_k, "qk_norm_rope_bwd: one of the gains' gradients is null");
   LS_REQUIRE(!dgain_q || (gain_q && gain_k), "qk_norm_rope_bwd: gradients of gains that are not there");
   LS_REQUIRE(!dgain_q || partial, "qk_norm_rope_bwd: null partial");
+  LS_REQUIRE(!dgain_q || dgain_q != dgain_k, "qk_norm_rope_bwd: the gains' gradients share one place");
   hipStream_t st = (hipStream_t)stream;
   s.norm = s.norm == 1;
   int blocks = bwd_blocks((long)T * h);

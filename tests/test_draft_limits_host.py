@@ -167,3 +167,11 @@ def test_stage_verify_looks_at_its_arrays(host_calls):
         with pytest.raises(AssertionError, match=text):
             call(**over)
     assert len(host_calls) == 1
+
+
+def test_the_gradients_of_both_gains_need_a_place_each():
+    def call(dgq, dgk):
+        return Bd.lib().lsk_qk_norm_rope_bwd(P, 384, 2 * P, 384, 3 * P, 384, Bd.LS_F16, 4, 4, 1, 64, 1, P, P, Bd.LS_F16, 1e-5, 64, 0, P, P, 16,
+                                             dgq, dgk, 0, None, P, None)
+
+    assert call(4 * P, 4 * P) == Bd.LS_EINVAL and "one place" in Bd.lib().ls_last_error().decode()
