@@ -1037,7 +1037,6 @@ ls_status lsk_attn_tree(const void* q, long ldq, int dt, int T, int B, int max_n
                         const int32_t* start, const int32_t* ctx_len, const uint64_t* mask, const void* k_pool,
                         const void* v_pool, const int32_t* block_table, int max_pages, int page, int n_pages, int max_ctx,
                         void* o, long ldo, float* scratch, size_t scratch_floats, void* stream) {
-  LsTimed timed(LSK_TIMED_DECODE_ATTN, stream);
   LS_REQUIRE(q && start && ctx_len && mask && k_pool && v_pool && block_table && o, "attn_tree: null argument");
   LS_REQUIRE(dt == LS_F32 || dt == LS_BF16 || dt == LS_F16, "attn_tree: unknown dtype %d", dt);
   LS_REQUIRE(T > 0 && B > 0 && h > 0 && hk > 0 && max_pages > 0 && page > 0 && n_pages > 0 && max_ctx >= 0,
@@ -1095,6 +1094,7 @@ ls_status lsk_attn_tree(const void* q, long ldq, int dt, int T, int B, int max_n
       else if (dh == 64) rows(one_, std::integral_constant<int, 64>());
       else rows(one_, std::integral_constant<int, 128>());
     };
+    LsTimed timed(LSK_TIMED_DECODE_ATTN, stream);   // a refusal launches nothing and is not recorded
     if (dt == LS_F32) size((float*)nullptr);
     else if (dt == LS_BF16) size((bf16_t*)nullptr);
     else size((f16_t*)nullptr);
@@ -1107,6 +1107,7 @@ ls_status lsk_attn_tree(const void* q, long ldq, int dt, int T, int B, int max_n
     tree_attn_any_kernel<T_><<<dim3((unsigned)T, h), 256, 0, st>>>((const T_*)q, ldq, (T_*)o, ldo, (const T_*)k_pool,
                                                                   (const T_*)v_pool, tr, h, hk, dh, scale_log2);
   };
+  LsTimed timed(LSK_TIMED_DECODE_ATTN, stream);
   if (dt == LS_F32) any((float*)nullptr);
   else if (dt == LS_BF16) any((bf16_t*)nullptr);
   else any((f16_t*)nullptr);

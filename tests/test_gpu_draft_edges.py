@@ -93,3 +93,18 @@ def test_scratch_of_another_stream_is_no_block_of_the_current_one():
     at = s.data_ptr()
     del s
     assert Bd._scratch(n, t, torch.cuda.current_stream()).data_ptr() == at
+
+
+def test_a_refused_call_is_not_recorded_by_the_launch_timing():
+    c = Case(24, [9], [3], 1, 1, 64, 16, "f16")
+    q = c.q.cuda()
+    Bd.lsk_timing_begin()
+    with pytest.raises(Bd.LsError, match="evenly"):
+        Bd._check(Bd.lib().lsk_attn_tree(q.data_ptr(), 192, Bd.LS_F16, 3, 1, 3, 3, 2, 64, *[q.data_ptr()] * 6, 1, 16, 1, 9, q.data_ptr(), 192,
+                                         None, 0, None))
+    assert Bd.lsk_timing_end()["decode_attn"][1] == 0
+    Bd.lsk_timing_begin()
+    c.run(q=q)
+    Bd.lsk_attn_tree(q, torch.empty_like(q), 1, 1, 64, i32(c.start), i32(c.past), c.mask(), 3, c.kp.cuda()[..., :12, :].contiguous(),
+                     c.vp.cuda()[..., :12, :].contiguous(), i32(c.bt), 12, 9)      # pages that are no power of two: the other kernel
+    assert Bd.lsk_timing_end()["decode_attn"][1] == 2
