@@ -108,3 +108,102 @@ def test_a_refused_call_is_not_recorded_by_the_launch_timing():
     Bd.lsk_attn_tree(q, torch.empty_like(q), 1, 1, 64, i32(c.start), i32(c.past), c.mask(), 3, c.kp.cuda()[..., :12, :].contiguous(),
                      c.vp.cuda()[..., :12, :].contiguous(), i32(c.bt), 12, 9)      # pages that are no power of two: the other kernel
     assert Bd.lsk_timing_end()["decode_attn"][1] == 2
+
+
+def kept_keys(c, b, t, gone):
+    """Keys that row t of request b sees: cached tokens and its mask's nodes, none of them on the table's entries `gone`."""
+    p = c.past[b]
+    return np.array([j for j in list(range(p)) + [p + i for i in c.seen[t]] if j // c.page not in gone], np.int64)
+
+
+def check_rows(c, o, rows, gone=()):
+    """The given rows of request 0 against 64 bits, over the keys that are there."""
+    q, kp, vp, got = f64(c.q), f64(c.kp), f64(c.vp), f64(o)
+    half = D.HALF[c.dtype] if c.dtype != "f32" else 2 * D.F32
+    for t in rows:
+        j = kept_keys(c, 0, t, gone)
+        for head in range(c.h):
+            at = c.bt[0, j // c.page], head // (c.h // c.hk), j % c.page
+            cols = slice(head * c.dh, (head + 1) * c.dh)
+            ref, tol = D.attend(q[t, cols], kp[at], vp[at], np.arange(len(j)), c.dtype, half)
+            assert (np.abs(got[t, cols] - ref) <= tol).all(), (t, head)
+
+
+# nodes, heads and key heads as in ROWS; a tile of 64 keys holds nodes in both halves: the context ends at 52 of 64
+@pytest.mark.parametrize("value", [float("nan"), float("inf"), -float("inf")])
+@pytest.mark.parametrize("nodes,h,hk", ROWS)
+@pytest.mark.parametrize("dtype,dh", [("f16", 64), ("bf16", 128), ("bf16", 32), ("f32", 64), ("f16", 80)])
+def test_values_that_are_not_finite_reach_the_rows_that_see_them(dtype, dh, nodes, h, hk, value):
+    past = 692
+    bad = [2, nodes - 2]                             # slots 694 and, from 24 nodes on, one of the next tile
+    rng = np.random.default_rng(31)
+    seen = [sorted({i} | set(np.flatnonzero(rng.random(nodes) < 0.4).tolist())) for i in range(nodes)]
+    sees = [t for t in range(nodes) if set(bad) & set(seen[t])]
+    blind = [t for t in range(nodes) if t not in sees]
+    assert len(blind) >= 2 and len(sees) >= 2
+    some = blind[::max(1, len(blind) // 4)]
+    for scratch in (None, torch.empty(0, device="cuda")):      # the context in parts, and whole
+        c = Case(31, [past], [nodes], h, hk, dh, 16, dtype, seen=seen)
+        for i in bad:
+            c.vp[c.bt[0, (past + i) // 16], :, (past + i) % 16] = value
+        o = c.run(scratch=scratch)
+        check_rows(c, o, some)
+        hit = o[sees].float()
+        assert torch.isnan(hit).all() if np.isnan(value) else (hit == value).all()
+        for i in bad:
+            c.kp[c.bt[0, (past + i) // 16], :, (past + i) % 16] = value
+        o = c.run(scratch=scratch)
+        check_rows(c, o, some)
+        assert not torch.isfinite(o[sees].float()).any()
+
+
+@pytest.mark.parametrize("nodes,h,hk", ROWS)
+@pytest.mark.parametrize("dtype,dh", [("f16", 64), ("bf16", 128), ("bf16", 32), ("f32", 64), ("f16", 80)])
+def test_missing_pages_of_the_context_and_of_the_nodes(dtype, dh, nodes, h, hk):
+    past = 692                                       # pages 0 .. 42, four tokens of page 43 and the nodes behind them
+    for gone in ((5,), (0, 1, 2, 3), (20, 43), (42, 44)):
+        c = Case(32, [past], [nodes], h, hk, dh, 16, dtype)
+        bt = c.bt.copy()
+        for i, p in enumerate(g for g in gone if g < bt.shape[1]):
+            bt[0, p] = -1 if i % 2 else c.n_pages
+        for scratch in (None, torch.empty(0, device="cuda")):
+            o = c.run(bt=i32(bt), scratch=scratch)
+            check_rows(c, o, range(0, nodes, max(1, nodes // 5)), gone)
+            assert torch.isfinite(o.float()).all()
+
+
+@pytest.mark.parametrize("nodes", [8, 24])
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("dh", [32, 64, 128])
+def test_weights_of_few_rows_come_in_two_parts(dh, dtype, nodes):
+    """Up to 32 rows the softmax weights enter the product rounded and as a remainder, each of 16 bits.  Outputs are made nearly
+    zero by cancellation, so that their own rounding hides nothing: weights rounded once would be outside the bound."""
+    past = 40
+    c = Case(33, [past], [nodes], 1, 1, dh, 16, dtype, seen=[[i] for i in range(nodes)])
+    c.q[:, 2:] = 0                                   # scores of two products each
+    q, kp, vp = f64(c.q), f64(c.kp), f64(c.vp)
+    slot = lambda j: (c.bt[0, j // 16], 0, j % 16)   # noqa: E731
+    seen = [np.array(list(range(past)) + [past + t]) for t in range(nodes)]
+    scores = [kp[slot(seen[t])] @ q[t] / np.sqrt(dh) for t in range(nodes)]
+    weights = [np.exp(s - s.max()) / np.exp(s - s.max()).sum() for s in scores]
+    # dimension d is balanced for row d % nodes by the value of that row's own key
+    for d in range(dh):
+        t = d % nodes
+        v = vp[slot(seen[t])][:, d]
+        c.vp[slot(past + t) + (d,)] = float(np.clip(-(weights[t][:-1] @ v[:-1]) / weights[t][-1], -1e3, 1e3))
+    vp, got = f64(c.vp), f64(c.run())
+    once = 0
+    for t in range(nodes):
+        v, w, s = vp[slot(seen[t])], weights[t], scores[t]
+        ref, mag = w @ v, w @ np.abs(v)
+        # a remainder is at most HALF of its weight and is rounded by HALF of itself; the score is two exact products, their sum,
+        # the scaling and the exponential's argument; sums over the keys in fp32
+        rel = D.HALF[dtype] ** 2 + 2 * 8 * D.F32 * max(1.0, np.abs(s).max()) + (len(w) / 4 + 80) * D.F32
+        tol = 1.01 * rel * mag + 1.01 * D.HALF[dtype] * np.abs(ref) + 2.0 ** -24 * (dtype == "f16")
+        if dtype == "f16":                           # parts below 2^-20 of the largest weight are subnormal, and lost
+            tol = tol + 2.0 ** -20 * w.max() * np.abs(v).sum(0)
+        assert (np.abs(got[t] - ref) <= tol).all(), (t, float((np.abs(got[t] - ref) / tol).max()))
+        p = torch.from_numpy(np.exp(s - s.max()).astype(np.float32))
+        single = (f64(p.to(DT[dtype])) @ v) / f64(p).sum()
+        once += int((np.abs(single - ref) > tol).sum())
+    assert once > dh // 8
