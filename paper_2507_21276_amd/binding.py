@@ -659,10 +659,11 @@ def _at(t):
 
 
 def _rows(t, T, width):
-    """Pointer and row distance of a matrix of T rows of at least width elements, dense within a row."""
+    """Pointer and row distance of a matrix of T rows of at least width elements, dense within a row (width for a single row,
+    whose stride means nothing)."""
     (n, w), (ld, one) = t.shape, t.stride()
     assert n == T and w >= width and (one == 1 or w == 1), "rows must be dense and wide enough"
-    return t.data_ptr(), ld if n > 1 else w
+    return t.data_ptr(), ld if n > 1 else width
 
 
 def _indexes(t, n):
@@ -750,16 +751,17 @@ def lsk_qk_norm_rope_kv_write(qkv, q_out, n_heads, n_kv_heads, head_dim, pos, re
     """q of qkv, normalised and rotated, to q_out; k and v to their slots of the pools [n_pages, n_kv_heads, page, head_dim]."""
     (T, w), (ld, one) = qkv.shape, qkv.stride()
     (T_q, w_q), (ld_q, one_q) = q_out.shape, q_out.stride()
-    dtype = qkv.dtype
-    assert T == T_q and one == 1 == one_q and w >= (n_heads + 2 * n_kv_heads) * head_dim and w_q >= n_heads * head_dim, \
-        "rows must be dense and wide enough"
+    dtype, width = qkv.dtype, (n_heads + 2 * n_kv_heads) * head_dim
+    assert T == T_q and one == 1 == one_q and w >= width and w_q >= n_heads * head_dim, "rows must be dense and wide enough"
+    if T == 1:   # the strides of a single row mean nothing
+        ld = ld_q = width
     assert q_out.dtype is dtype and _same_pools(k_pool, v_pool, (n_kv_heads, page_size, head_dim), dtype)
     assert block_table.dtype is _INT and block_table.is_contiguous()
     dev = qkv.get_device()
     assert q_out.get_device() == dev == k_pool.get_device() and v_pool.get_device() == dev == block_table.get_device() \
         and req.get_device() == dev and (slot is None or slot.get_device() == dev), "tensors on different devices"
     _check(lib().lsk_qk_norm_rope_kv_write(
-        qkv.data_ptr(), ld if T > 1 else w, q_out.data_ptr(), ld_q if T > 1 else w_q, CODE_OF_TORCH[dtype], T, n_heads, n_kv_heads,
+        qkv.data_ptr(), ld, q_out.data_ptr(), ld_q, CODE_OF_TORCH[dtype], T, n_heads, n_kv_heads,
         head_dim, *_norm_rope(dev, T, head_dim, gain_q, gain_k, norm, eps, pos, table, layout), _indexes(req, T), _indexes(slot, T),
         k_pool.data_ptr(), v_pool.data_ptr(), block_table.data_ptr(), block_table.shape[1], page_size, k_pool.shape[0],
         _here(stream, dev)))
@@ -782,6 +784,8 @@ def lsk_attn_tree(q, o, n_heads, n_kv_heads, head_dim, start, ctx_len, mask, max
     n_rows, per_row = block_table.shape
     B, dtype, L, at = start.numel() - 1, q.dtype, lib(), None
     assert T == T_o and one == 1 == one_o and w >= n_heads * head_dim <= w_o, "rows must be dense and wide enough"
+    if T == 1:
+        ld = ld_o = n_heads * head_dim
     assert o.dtype is dtype and _same_pools(k_pool, v_pool, (n_kv_heads, page_size, head_dim), dtype)
     assert mask.shape == (T, (max_nodes + 63) // 64) and mask.element_size() == 8 and mask.is_contiguous()
     assert n_rows >= B and block_table.dtype is _INT and block_table.is_contiguous(), "a row of page ids for each request"
@@ -800,9 +804,9 @@ def lsk_attn_tree(q, o, n_heads, n_kv_heads, head_dim, start, ctx_len, mask, max
             scratch = _scratch(n, q, stream)
             at = scratch.data_ptr()
     _check(L.lsk_attn_tree(
-        q.data_ptr(), ld if T > 1 else w, CODE_OF_TORCH[dtype], T, B, max_nodes, n_heads, n_kv_heads, head_dim, _indexes(start, 2),
+        q.data_ptr(), ld, CODE_OF_TORCH[dtype], T, B, max_nodes, n_heads, n_kv_heads, head_dim, _indexes(start, 2),
         _indexes(ctx_len, B), mask.data_ptr(), k_pool.data_ptr(), v_pool.data_ptr(), block_table.data_ptr(), per_row, page_size,
-        k_pool.shape[0], max_ctx, o.data_ptr(), ld_o if T > 1 else w_o, at, n,
+        k_pool.shape[0], max_ctx, o.data_ptr(), ld_o, at, n,
         _here(stream, dev)))
 
 

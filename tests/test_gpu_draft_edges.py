@@ -207,3 +207,27 @@ def test_weights_of_few_rows_come_in_two_parts(dh, dtype, nodes):
         single = (f64(p.to(DT[dtype])) @ v) / f64(p).sum()
         once += int((np.abs(single - ref) > tol).sum())
     assert once > dh // 8
+
+
+@pytest.mark.parametrize("T", [1, 2])
+def test_q_in_place_of_its_columns_of_the_projection(T):
+    """q_out is the q columns of qkv, for one row as for several; so are q and o of the attention a part of wider rows."""
+    h, hk, dh, page = 4, 2, 64, 16
+    g = torch.Generator()
+    g.manual_seed(41)
+    x = torch.randn(T, (h + 2 * hk) * dh, generator=g).half().cuda()
+    kp, vp = (torch.zeros(1, hk, page, dh, dtype=torch.float16, device="cuda") for _ in range(2))
+    table = torch.from_numpy(D.table(16, dh)).cuda()
+    args = (h, hk, dh, i32(range(T)), i32([0] * T), kp, vp, i32([[0]]), page)
+    want = torch.empty(T, h * dh, dtype=torch.float16, device="cuda")
+    Bd.lsk_qk_norm_rope_kv_write(x, want, *args, table=table)
+    k = kp.clone()
+    y = x.clone()
+    Bd.lsk_qk_norm_rope_kv_write(y, y[:, :h * dh], *args, table=table)
+    assert torch.equal(y[:, :h * dh], want) and torch.equal(y[:, h * dh:], x[:, h * dh:]) and torch.equal(kp, k)
+    mask = torch.tensor([[(2 << t) - 1] for t in range(T)], device="cuda")
+    tree = (h, hk, dh, i32([0, T]), i32([0]), mask, T, kp, vp, i32([[0]]), page, 0)
+    o, wide = torch.empty_like(want), torch.full((T, h * dh + 3), 7.0, dtype=torch.float16, device="cuda")
+    Bd.lsk_attn_tree(want, o, *tree)
+    Bd.lsk_attn_tree(y[:, :h * dh], wide[:, :h * dh], *tree)
+    assert torch.allclose(wide[:, :h * dh].float(), o.float(), rtol=2 ** -9, atol=2 ** -12) and (wide[:, h * dh:] == 7).all()
