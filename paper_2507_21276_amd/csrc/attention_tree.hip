@@ -414,11 +414,13 @@ __global__ __launch_bounds__(256, DH == 64 && RW == 1 ? 3 : 2) void tree_attn_ke
   const int v_put = v_at<DH>(lane / LPR, lane % LPR) + rw * NL * 1024;
   const int v_get = v_at<DH>(4 * quad + (col >> 2), (col >> 1) & 1) + (col & 1) * 8, k_get = k_at<DH>(col, quad);
   auto v_put_at = [&](int j) { return (v_put ^ (DH == 128 ? (j & 1) << 7 : 0)) + j * 1024; };
-  // Tiles of which all rows see all keys are taken as they are.  There an infinite value times a weight that 16 bits do not hold, or
-  // times the remainder of one, is NaN where the weight itself, which is positive, gives infinity: results that are not finite are
-  // computed once more, with every tile looked through.  (Finite ones: 0 - 2 % for the registers that the way back takes.)
+  // Tiles of which all rows see all keys are taken as they are.  There an infinite value times the remainder of a weight (SPLIT below),
+  // or times one that fp16 does not hold, is NaN where the weight itself, which is positive, gives infinity: results that are not
+  // finite are computed once more, with every tile looked through.  (Finite ones: 0 - 2 % for the registers that the way back takes, 5 %
+  // for 24 rows of head_dim 64.  bf16 weights rounded once have fp32's range: nothing to look for.)
+  constexpr bool AGAIN = RW == 1 || std::is_same_v<T, f16_t>;
   bool looked = false;
-  auto is_plain = [&](int t, int bad) { return !looked && (t + 1) * KEYS <= ctx && (t + 1) * KEYS <= k_hi && bad == 0; };
+  auto is_plain = [&](int t, int bad) { return !(AGAIN && looked) && (t + 1) * KEYS <= ctx && (t + 1) * KEYS <= k_hi && bad == 0; };
   auto all_finite = [&] {
     float x = 0.f;
 #pragma unroll
@@ -720,7 +722,7 @@ __global__ __launch_bounds__(256, DH == 64 && RW == 1 ? 3 : 2) void tree_attn_ke
     for (;;) {
       clear();
       t = t_lo;
-      asm volatile("" : "+s"(t));
+      if constexpr (AGAIN) asm volatile("" : "+s"(t));
       t += kw;
       bad = 0;
       ids = look_up(t);
@@ -735,7 +737,7 @@ __global__ __launch_bounds__(256, DH == 64 && RW == 1 ? 3 : 2) void tree_attn_ke
         if ((i += KW) >= t_hi) break;
         step(smem2, smem, 1);
       }
-      if (looked || !__syncthreads_or(!all_finite())) break;
+      if (!AGAIN || looked || !__syncthreads_or(!all_finite())) break;
       looked = true;
     }
   }
