@@ -102,8 +102,8 @@ ls_status lsk_rope_table(float* table, int n_pos, int rot_dim, float theta, cons
  * and v is copied.  out may be in (equal ld; v stays) but must not overlap it otherwise.  layout LSK_ROPE_HALF: the pairs
  * (i, i + rot_dim/2), as lsk_rope; LSK_ROPE_NEIGHBOURS: (2i, 2i + 1).  table [dev] [max_pos][rot_dim/2][cos, sin];
  * positions outside 0..max_pos-1 take the nearest row.  head_dim even, 2..512; rot_dim even, at most head_dim.  fp32
- * arithmetic, one rounding.  head_dim and rot_dim multiples of 8 with rows and bases aligned to four elements take the
- * vectorised kernels.
+ * arithmetic, one rounding.  Multiples of 8 as head_dim, up to 256, and rot_dim with rows and bases aligned to four elements
+ * take the vectorised kernels.
  */
 enum { LSK_ROPE_HALF = 0, LSK_ROPE_NEIGHBOURS = 1 };
 ls_status lsk_qk_norm_rope(const void* in, long ld_in, void* out, long ld_out, int dtype, int T, int n_heads,
@@ -331,7 +331,8 @@ ls_status lsk_attn_paged_noalloc(const void* qkv, int dtype, int T, int n_heads,
 /*
  * The serving form of lsk_qk_norm_rope: q goes to q_out [dev] (rows ld_q elements apart; may be qkv with ld_q = ld), the k
  * and v rows to slot slot[t] (null: pos[t]) of request req[t]'s pages, pools [n_pages][n_kv_heads][page_size][head_dim] of
- * dtype; k and v of qkv stay as they are.  The slot differs from the position for drafted tokens: nodes of one depth share
+ * dtype; k and v of qkv stay as they are.  q is rounded to dtype between this call and the attention, as the stage's other
+ * serving calls round it: in bf16 that adds as much to the attention's error as the result's own rounding.  The slot differs from the position for drafted tokens: nodes of one depth share
  * a position.  Rows with req[t] < 0 are padding and are skipped; K and V of a slot beyond the block-table row, or of a page
  * id outside 0..n_pages-1, are not written.  No two rows may share a slot.
  */

@@ -337,6 +337,7 @@ class Stage:
         for x in (X, Y):
             assert x is None or x.dtype is self.io_torch and x.numel() >= T * self.c.d_model, "rows of the stage's io type, one a node"
         assert kv.block_table.shape[0] >= B <= kv.ctx_len.numel(), "a row of page ids and a length for each request"
+        _device(kv.k_pool, kv.v_pool, kv.block_table, kv.ctx_len, X, Y, parent, start)
         d = kv.desc(with_host)
         _check(lib().stage_verify(self.h, _p(X), _indexes(parent, T), _indexes(start, B + 1), n, B, C.byref(d), _p(Y), _p(workspace),
                                   _stream(stream)))

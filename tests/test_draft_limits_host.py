@@ -166,6 +166,10 @@ def test_stage_verify_looks_at_its_arrays(host_calls):
                        (dict(X=z(5, 16, t=torch.bfloat16)), "io type"), (dict(table=z(1, 4)), "page ids"), (dict(ctx=(0,)), "length")):
         with pytest.raises(AssertionError, match=text):
             call(**over)
+    for name in ("X", "Y", "parent", "start"):
+        there = dict(X=z(5, 16, **F32), Y=z(5, 16, **F32), parent=z(5), start=z(3))[name].as_subclass(Elsewhere)
+        with pytest.raises(AssertionError, match="device"):
+            call(**{name: there})
     assert len(host_calls) == 1
 
 
