@@ -331,10 +331,11 @@ ls_status lsk_attn_paged_noalloc(const void* qkv, int dtype, int T, int n_heads,
 /*
  * The serving form of lsk_qk_norm_rope: q goes to q_out [dev] (rows ld_q elements apart; may be qkv with ld_q = ld), the k
  * and v rows to slot slot[t] (null: pos[t]) of request req[t]'s pages, pools [n_pages][n_kv_heads][page_size][head_dim] of
- * dtype; k and v of qkv stay as they are.  q is rounded to dtype between this call and the attention, as the stage's other
- * serving calls round it: in bf16 that adds as much to the attention's error as the result's own rounding.  The slot differs from the position for drafted tokens: nodes of one depth share
- * a position.  Rows with req[t] < 0 are padding and are skipped; K and V of a slot beyond the block-table row, or of a page
- * id outside 0..n_pages-1, are not written.  No two rows may share a slot.
+ * dtype; k and v of qkv stay as they are.  q is rounded to dtype between this call and the attention, as in the stage's other
+ * serving calls: in bf16 that adds as much to the attention's error as the result's own rounding does.  The slot differs from
+ * the position for drafted tokens: nodes of one depth share a position.  Rows with req[t] < 0 are padding and are skipped; K
+ * and V of a slot beyond the block-table row, or of a page id outside 0..n_pages-1, are not written.  No two rows may share a
+ * slot.
  */
 ls_status lsk_qk_norm_rope_kv_write(const void* qkv, long ld, void* q_out, long ld_q, int dtype, int T, int n_heads,
                                     int n_kv_heads, int head_dim, int kind, const void* gain_q, const void* gain_k,
