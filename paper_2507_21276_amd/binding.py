@@ -644,10 +644,12 @@ def _here(stream, dev):
 def _scratch(n, t, stream):
     """n floats beside t for a call on that stream.  They are the stream's own: a block of the current stream's could still be in
     use by that stream's earlier work, which this one does not wait for, and could go to its later work too soon."""
-    raw = None if stream is None else _stream(stream) or 0
-    if raw is None or raw == torch._C._cuda_getCurrentRawStream(t.get_device()):
+    if stream is not None and not isinstance(stream, torch.cuda.Stream):
+        raw = int(stream)   # 0, the default stream, is no external one
+        stream = torch.cuda.ExternalStream(raw, t.device) if raw else torch.cuda.default_stream(t.device)
+    if stream is None or stream.cuda_stream == torch._C._cuda_getCurrentRawStream(t.get_device()):
         return torch.empty(n, dtype=torch.float32, device=t.device)
-    with torch.cuda.stream(stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(raw, t.device)):
+    with torch.cuda.stream(stream):
         return torch.empty(n, dtype=torch.float32, device=t.device)
 
 

@@ -231,3 +231,16 @@ def test_q_in_place_of_its_columns_of_the_projection(T):
     Bd.lsk_attn_tree(want, o, *tree)
     Bd.lsk_attn_tree(y[:, :h * dh], wide[:, :h * dh], *tree)
     assert torch.allclose(wide[:, :h * dh].float(), o.float(), rtol=2 ** -9, atol=2 ** -12) and (wide[:, h * dh:] == 7).all()
+
+
+def test_scratch_of_the_default_stream_from_within_another():
+    n, t, side = 3 << 20, torch.empty(1, device="cuda"), torch.cuda.Stream()
+    for stream in (0, torch.cuda.default_stream()):
+        torch.cuda.synchronize()
+        torch.cuda.empty_cache()
+        with torch.cuda.stream(side):
+            s = Bd._scratch(n, t, stream)
+            at = s.data_ptr()
+            del s
+            assert torch.empty(n, device="cuda").data_ptr() != at
+        assert torch.empty(n, device="cuda").data_ptr() == at      # the default stream's block again
