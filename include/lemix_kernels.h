@@ -362,11 +362,11 @@ ls_status lsk_qk_norm_rope_kv_write(const void* qkv, long ld, void* q_out, long 
  * beyond the block-table row or of a page id outside 0..n_pages-1 are not seen.  Slots that no row sees, and keys of nodes
  * that a row does not see, may hold any bit pattern.  Rows from start[B] on, and nodes from max_nodes on, are left as they were.
  * max_ctx [host]: the largest ctx_len, for launch sizing.  scratch [dev]: fp32 for the partial results of contexts that are
- * split over workgroups; lsk_attn_tree_scratch_floats gives the most a call uses, up to 2^28 (1 GB), fewer (scratch_floats; 0
- * with null) mean fewer parts.  head_dim up to 256; head_dim 32, 64 or 128 with page_size a power of two from 8 on, and q, o, pools, rows and
- * scratch aligned to 16 bytes take the matrix-core kernels.  Two calls that overlap in time need two scratches.  LS_EINVAL, with
- * nothing launched, for more workgroups than a launch counts: 2^24 requests x key heads x blocks of rows (at most 128 rows of
- * max_nodes x query heads a key head), or 2^24 rows in the kernel for any size.
+ * split over workgroups; lsk_attn_tree_scratch_floats gives the most a call uses, up to 2^28 (1 GB), fewer (scratch_floats;
+ * 0 with null) mean fewer parts.  head_dim up to 256; head_dim 32, 64 or 128 with page_size a power of two from 8 on, and q, o,
+ * pools, rows and scratch aligned to 16 bytes take the matrix-core kernels.  Two calls that overlap in time need two scratches.
+ * LS_EINVAL, with nothing launched, for more workgroups than a launch counts: 2^24 requests x key heads x blocks of rows (at
+ * most 128 rows of max_nodes x query heads a key head), or 2^24 rows in the kernel for any size.
  */
 ls_status lsk_tree_index(const int32_t* parent, const int32_t* start, const int32_t* ctx_len, int B, int T, int max_nodes,
                          int32_t* pos, int32_t* slot, int32_t* req, uint64_t* mask, void* stream);

@@ -159,7 +159,7 @@ __global__ __launch_bounds__(256) void tree_attn_any_kernel(const T* q, long ldq
 //   well 239; two register sets of a tile and spills 330).
 //   RW = 2, 4 (more rows): bound by the exponentials and the products.  K and V tiles are loaded once for the RW wavefronts,
 //   straight to two LDS buffers and with one barrier a tile, of 64 keys where all four share it.  12 trees of 40 - 61 nodes, five
-//   query heads a key head, 3000 to 16001 tokens, with the join: 526 TFLOP/s (231 - 232 us; by way of registers, which are 32 more, 16
+//   query heads a key head, 3000 to 16001 tokens, with the join: 525 - 540 TFLOP/s (225 - 232 us by the card; by way of registers, which are 32 more, 16
 //   us longer; before that a wavefront with 64 rows of its own, which spills, 489; tiles of 32 keys 326); 64 of 64 nodes, 4096 tokens
 //   each, 467 us, by way of registers 500.  No single part sets the pace: of 238 us that a call alone took, 228 without the
 //   exponentials, 197 without the loads, 206 without the second product.

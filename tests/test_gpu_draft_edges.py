@@ -244,3 +244,27 @@ def test_scratch_of_the_default_stream_from_within_another():
             del s
             assert torch.empty(n, device="cuda").data_ptr() != at
         assert torch.empty(n, device="cuda").data_ptr() == at      # the default stream's block again
+
+
+def test_a_captured_call_with_scratch_of_its_own():
+    """The wrapper's scratch belongs to the graph: replays with eager calls and allocations of that size between them."""
+    c = Case(42, [3000, 1200], [9, 4], 4, 2, 128, 16, "bf16")
+    args = dict(kp=c.kp.cuda(), vp=c.vp.cuda(), bt=i32(c.bt), mask=c.mask(), start=i32(c.start), ctx=i32(c.past))
+    n = Bd.lib().lsk_attn_tree_scratch_floats(c.T, 2, 4, 2, 128, c.max_nodes, 3000)
+    assert n > 0
+    q, o = c.q.cuda(), torch.empty(c.T, 512, dtype=torch.bfloat16, device="cuda")
+    c.run(q=q, o=o, **args)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        c.run(q=q, o=o, **args)
+    g = torch.Generator(device="cuda")
+    g.manual_seed(2)
+    for _ in range(3):
+        q.normal_(generator=g)
+        others = [torch.full((n,), float("nan"), device="cuda") for _ in range(3)]
+        graph.replay()
+        want = c.run(q=q.clone(), **args)
+        torch.cuda.synchronize()
+        assert torch.equal(o, want)
+        del others
